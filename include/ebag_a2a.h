@@ -372,6 +372,82 @@ int ebag_a2a_queue_stream_destroy(hipStream_t stream);
 /* Release the plan's device memory.  NULL is ignored. */
 void ebag_a2a_destroy(ebag_a2a_t h);
 
+/*
+ * Tokens by expert: the mixture-of-experts side of the All-to-All.
+ *
+ * Each of N tokens has chosen `choices` experts; choice i = n * choices + j is
+ * token n's j-th.  The sort puts the S = N * choices choices in the order of
+ * their experts (by expert, then by choice number), the layout an All-to-All
+ * to the experts' owners and the experts' own products need; dispatch copies
+ * the tokens' rows into it and combine sums the experts' rows back:
+ *
+ *   pos[i]     the place of choice i in the order, a permutation of 0 .. S-1
+ *   src[p]     the choice at place p (src[pos[i]] == i)
+ *   offsets[e] the first place of expert e; offsets[experts] the number of
+ *              choices that an expert takes
+ *   dispatch:           xs[pos[n, j]] = x[n]
+ *   combine:            out[n] = sum_j weights[n, j] * ys[pos[n, j]]
+ *   combine backward:   dys[pos[n, j]] = weights[n, j] * dout[n],
+ *                       dweights[n, j] = <dout[n], ys[pos[n, j]]>
+ *   dispatch backward:  dx[n] = sum_j dxs[pos[n, j]]
+ *
+ * A choice whose expert number is outside [0, experts) is dropped: its place
+ * is behind every expert's (offsets[experts] <= pos), in choice order.  Dropped
+ * rows of xs and dys are zeros, dropped dweights are 0, and dropped rows of ys
+ * and dxs are not read, whatever they hold; a token without a kept choice gets
+ * a row of zeros.  Places must come from the sort (or be such a permutation);
+ * one outside [0, S) is treated as dropped, so nothing is read or written out
+ * of range.
+ *
+ * Rows are `dim` elements of type dtype (EBAG_F32, EBAG_F16, EBAG_BF16), any
+ * dim >= 1; row r of a matrix starts at element r * ld, ld >= dim, aligned to
+ * the element only (rows of whole 16-byte vectors on 16-byte boundaries are
+ * the fastest).  Weights and dweights are fp32 [N][choices].  Sums are fp32
+ * in the order j = 0, 1, ..., rounded once to dtype; every result is the same
+ * bits on every run.  Outputs must not overlap inputs.  N may be 0: only the
+ * sort's offsets are then written.
+ */
+typedef struct ebag_a2a_moe_plan* ebag_a2a_moe_t;
+
+/* Create a plan on the current HIP device for up to max_tokens tokens of
+ * `choices` choices each (1..64; max_tokens * choices below 2^31) and `experts`
+ * experts (1..512).  It owns the sort's counters (at most 264 KiB).  All calls
+ * must be made with the plan's device current (EBAG_EINVAL otherwise).  One
+ * sort may be in flight per plan, checked as the forward's is (EBAG_EBUSY);
+ * the other calls share nothing and may run on any stream.  All can be
+ * captured into a graph and replayed. */
+int ebag_a2a_moe_create(ebag_a2a_moe_t* out, int64_t max_tokens, int32_t choices, int32_t experts);
+
+/* Sort the choices: experts_of int32 [tokens][choices] -> offsets int32
+ * [experts + 1], pos int32 [tokens][choices], src int32 [tokens * choices].
+ * One launch up to 16384 choices, two above. */
+int ebag_a2a_moe_sort(ebag_a2a_moe_t h, const int32_t* experts_of, int64_t tokens, int32_t* offsets, int32_t* pos,
+                      int32_t* src, hipStream_t stream);
+
+/* Lay the tokens' rows x [tokens][dim] out by place: xs [tokens * choices][dim]. */
+int ebag_a2a_moe_dispatch(ebag_a2a_moe_t h, const void* x, int64_t ldx, int64_t dim, int32_t dtype, int64_t tokens,
+                          const int32_t* offsets, const int32_t* pos, void* xs, int64_t ldxs, hipStream_t stream);
+
+/* Gradient of dispatch: dx [tokens][dim] from dxs [tokens * choices][dim]. */
+int ebag_a2a_moe_dispatch_backward(ebag_a2a_moe_t h, const void* dxs, int64_t lddxs, int64_t dim, int32_t dtype,
+                                   int64_t tokens, const int32_t* offsets, const int32_t* pos, void* dx, int64_t lddx,
+                                   hipStream_t stream);
+
+/* Sum the experts' rows ys [tokens * choices][dim] into out [tokens][dim]. */
+int ebag_a2a_moe_combine(ebag_a2a_moe_t h, const void* ys, int64_t ldys, int64_t dim, int32_t dtype, int64_t tokens,
+                         const int32_t* offsets, const int32_t* pos, const float* weights, void* out, int64_t ldo,
+                         hipStream_t stream);
+
+/* Gradients of combine: dys [tokens * choices][dim] and dweights [tokens][choices]
+ * from dout [tokens][dim], in one pass over ys. */
+int ebag_a2a_moe_combine_backward(ebag_a2a_moe_t h, const void* dout, int64_t lddout, const void* ys, int64_t ldys,
+                                  int64_t dim, int32_t dtype, int64_t tokens, const int32_t* offsets,
+                                  const int32_t* pos, const float* weights, void* dys, int64_t lddys, float* dweights,
+                                  hipStream_t stream);
+
+/* Release the plan's device memory.  NULL is ignored. */
+void ebag_a2a_moe_destroy(ebag_a2a_moe_t h);
+
 /* Message for the calling thread's most recent failing call ("" if none). */
 const char* ebag_a2a_last_error(void);
 

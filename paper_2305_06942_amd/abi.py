@@ -85,6 +85,17 @@ _SIGS = {
     "ebag_a2a_queue_stream_destroy": ([_P], ctypes.c_int),
     "ebag_a2a_destroy": ([_P], None),
     "ebag_a2a_last_error": ([], ctypes.c_char_p),
+    "ebag_a2a_moe_create": ([_P, ctypes.c_int64, ctypes.c_int32, ctypes.c_int32], ctypes.c_int),
+    "ebag_a2a_moe_sort": ([_P, _P, ctypes.c_int64, _P, _P, _P, _P], ctypes.c_int),
+    "ebag_a2a_moe_dispatch": ([_P, _P, ctypes.c_int64, ctypes.c_int64, ctypes.c_int32, ctypes.c_int64, _P, _P, _P,
+                               ctypes.c_int64, _P], ctypes.c_int),
+    "ebag_a2a_moe_dispatch_backward": ([_P, _P, ctypes.c_int64, ctypes.c_int64, ctypes.c_int32, ctypes.c_int64, _P, _P,
+                                        _P, ctypes.c_int64, _P], ctypes.c_int),
+    "ebag_a2a_moe_combine": ([_P, _P, ctypes.c_int64, ctypes.c_int64, ctypes.c_int32, ctypes.c_int64, _P, _P, _P, _P,
+                              ctypes.c_int64, _P], ctypes.c_int),
+    "ebag_a2a_moe_combine_backward": ([_P, _P, ctypes.c_int64, _P, ctypes.c_int64, ctypes.c_int64, ctypes.c_int32,
+                                       ctypes.c_int64, _P, _P, _P, _P, ctypes.c_int64, _P, _P], ctypes.c_int),
+    "ebag_a2a_moe_destroy": ([_P], None),
     "gemv_ar_default_opts": ([_P], ctypes.c_int),
     "gemv_ar_create": ([_P, ctypes.c_int32, ctypes.c_int64, _P, ctypes.c_int32, _P], ctypes.c_int),
     "gemv_ar_forward": ([_P, _P, _P, _P, _P, _P], ctypes.c_int),
@@ -385,6 +396,111 @@ class Plan:
     def close(self):
         if getattr(self, "_h", None):
             self._lib.ebag_a2a_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+ROW_TYPES = {"float32": EBAG_F32, "float16": EBAG_F16, "bfloat16": EBAG_BF16}
+
+
+def _matrix(x, rows: int, cols: int, kind: Optional[str], what: str):
+    """(address, row step in elements, type name) of a matrix on the GPU: a
+    tensor [rows or more, cols] whose rows are contiguous, one step apart."""
+    name = _dtype_name(x.dtype)
+    if name not in ROW_TYPES or (kind is not None and name != kind):
+        raise ValueError(f"{what} must be {kind or ' or '.join(ROW_TYPES)}, not {name}")
+    if x.dim() != 2 or x.shape[0] < rows or x.shape[1] != cols:
+        raise ValueError(f"{what} must be [{rows}, {cols}], not {list(x.shape)}")
+    inner, step = x.stride(1), x.stride(0)
+    if (inner != 1 and cols > 1) or (step < cols and x.shape[0] > 1):
+        raise ValueError(f"{what} must have contiguous rows that do not overlap")
+    if not x.is_cuda:
+        raise ValueError(f"{what} must be a GPU tensor, not one on {x.device}")
+    return x.data_ptr(), (step if x.shape[0] > 1 else cols), name
+
+
+class MoePerm:
+    """A plan for sorting tokens by expert (``ebag_a2a_moe_create``): up to
+    max_tokens tokens of `choices` choices each, `experts` experts.  Methods
+    mirror the C ABI and take torch tensors: choices and places int32
+    [tokens, choices], offsets int32 [experts + 1], src int32 [tokens *
+    choices], weights float32 [tokens, choices], rows float32, float16 or
+    bfloat16 with any step between them."""
+
+    def __init__(self, max_tokens: int, choices: int, experts: int):
+        lib = load()
+        h = ctypes.c_void_p()
+        _check(lib.ebag_a2a_moe_create(ctypes.byref(h), int(max_tokens), int(choices), int(experts)))
+        self._h = h
+        self._lib = lib
+        self.choices, self.experts = int(choices), int(experts)
+
+    def _places(self, offsets, pos, weights=None, dweights=None) -> int:
+        """Checks what every call over rows shares; the number of tokens."""
+        _validate(((offsets,), "offsets", I32, None), ((pos,), "pos", I32, None), ((weights,), "weights", F32, None),
+                  ((dweights,), "dweights", F32, None))
+        tokens = pos.numel() // self.choices
+        if pos.numel() != tokens * self.choices:
+            raise ValueError(f"pos must be [tokens, {self.choices}], not {list(pos.shape)}")
+        _need(offsets, 4 * (self.experts + 1), "offsets")
+        _need(weights, 4 * pos.numel(), "weights")
+        _need(dweights, 4 * pos.numel(), "dweights")
+        return tokens
+
+    def sort(self, experts_of, offsets, pos, src, stream=None):
+        _validate(((experts_of,), "experts_of", I32, None), ((offsets,), "offsets", I32, None),
+                  ((pos,), "pos", I32, None), ((src,), "src", I32, None))
+        n = experts_of.numel()
+        if n % self.choices:
+            raise ValueError(f"experts_of must be [tokens, {self.choices}], not {list(experts_of.shape)}")
+        _need(offsets, 4 * (self.experts + 1), "offsets")
+        _need(pos, 4 * n, "pos")
+        _need(src, 4 * n, "src")
+        _check(self._lib.ebag_a2a_moe_sort(self._h, experts_of.data_ptr(), n // self.choices, offsets.data_ptr(),
+                                           pos.data_ptr(), src.data_ptr(), _stream(stream)))
+
+    def dispatch(self, x, offsets, pos, xs, stream=None):
+        n = self._places(offsets, pos)
+        dim = x.shape[-1]
+        px, ldx, kind = _matrix(x, n, dim, None, "x")
+        pxs, ldxs, _ = _matrix(xs, n * self.choices, dim, kind, "xs")
+        _check(self._lib.ebag_a2a_moe_dispatch(self._h, px, ldx, dim, ROW_TYPES[kind], n, offsets.data_ptr(),
+                                               pos.data_ptr(), pxs, ldxs, _stream(stream)))
+
+    def dispatch_backward(self, dxs, offsets, pos, dx, stream=None):
+        n = self._places(offsets, pos)
+        dim = dxs.shape[-1]
+        ps, lds, kind = _matrix(dxs, n * self.choices, dim, None, "dxs")
+        pd, ldd, _ = _matrix(dx, n, dim, kind, "dx")
+        _check(self._lib.ebag_a2a_moe_dispatch_backward(self._h, ps, lds, dim, ROW_TYPES[kind], n, offsets.data_ptr(),
+                                                        pos.data_ptr(), pd, ldd, _stream(stream)))
+
+    def combine(self, ys, offsets, pos, weights, out, stream=None):
+        n = self._places(offsets, pos, weights)
+        dim = ys.shape[-1]
+        py, ldy, kind = _matrix(ys, n * self.choices, dim, None, "ys")
+        po, ldo, _ = _matrix(out, n, dim, kind, "out")
+        _check(self._lib.ebag_a2a_moe_combine(self._h, py, ldy, dim, ROW_TYPES[kind], n, offsets.data_ptr(),
+                                              pos.data_ptr(), weights.data_ptr(), po, ldo, _stream(stream)))
+
+    def combine_backward(self, dout, ys, offsets, pos, weights, dys, dweights, stream=None):
+        n = self._places(offsets, pos, weights, dweights)
+        dim = ys.shape[-1]
+        pd, ldd, kind = _matrix(dout, n, dim, None, "dout")
+        py, ldy, _ = _matrix(ys, n * self.choices, dim, kind, "ys")
+        ps, lds, _ = _matrix(dys, n * self.choices, dim, kind, "dys")
+        _check(self._lib.ebag_a2a_moe_combine_backward(self._h, pd, ldd, py, ldy, dim, ROW_TYPES[kind], n,
+                                                       offsets.data_ptr(), pos.data_ptr(), weights.data_ptr(), ps, lds,
+                                                       dweights.data_ptr(), _stream(stream)))
+
+    def close(self):
+        if getattr(self, "_h", None):
+            self._lib.ebag_a2a_moe_destroy(self._h)
             self._h = None
 
     def __del__(self):

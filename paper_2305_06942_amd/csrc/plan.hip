@@ -15,6 +15,7 @@
 #include "backward.h"
 #include "consume.h"
 #include "device_guard.h"
+#include "in_flight.h"
 
 using namespace ebag;
 
@@ -71,14 +72,6 @@ int ebag::xcd_count(int num_cus) { return (num_cus % 32 == 0 && num_cus >= 64) ?
 int32_t ebag::table_groups_for(const ebag_a2a_opts_t& o, int32_t T, int n_xcd) {
   return o.table_major == 2 ? 1 : o.table_major == 1 ? (T % n_xcd == 0 ? n_xcd : 1) : 0;
 }
-
-// One kind of call whose device state a plan shares between calls: the
-// event recorded after the last one and the stream it was enqueued on.
-struct InFlight {
-  hipEvent_t done = nullptr;
-  hipStream_t stream = nullptr;
-  bool pending = false;
-};
 
 struct ebag_a2a_plan {
   int device = 0;
@@ -239,40 +232,6 @@ int sync_tables(ebag_a2a_plan* h, const void* const* tables, hipStream_t stream)
   }
   std::memcpy(h->host_tables.data(), tables, sizeof(void*) * h->T);
   h->tables_valid = true;
-  return EBAG_OK;
-}
-
-// Whether `stream` is being captured into a graph.  Work that waits for a
-// host-chosen epoch cannot be replayed from a graph: the epoch is fixed at
-// capture, so a replay would not wait for the flags of its own producer.
-bool capturing(hipStream_t stream) {
-  hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
-  return hipStreamIsCapturing(stream, &cs) == hipSuccess && cs != hipStreamCaptureStatusNone;
-}
-
-// One call of each kind in flight per plan: a call on another stream than
-// the last one of its kind, while that one has not completed, would share its
-// device state.
-int check_busy(InFlight& f, hipStream_t stream, const char* what) {
-  if (!f.pending || stream == f.stream || capturing(stream)) return EBAG_OK;
-  const hipError_t e = hipEventQuery(f.done);
-  if (e == hipErrorNotReady)
-    return fail(EBAG_EBUSY, "a %s of this plan is still running on another stream (the plan's device state for it "
-                            "is shared): order them on one stream or wait for it", what);
-  if (e != hipSuccess) return hip_fail(e, "query the last call");
-  f.pending = false;
-  return EBAG_OK;
-}
-
-// Remember the call just enqueued on `stream` (not under graph capture).
-int note_call(InFlight& f, hipStream_t stream) {
-  if (capturing(stream)) {
-    f.pending = false;
-    return EBAG_OK;
-  }
-  HIP_TRY(hipEventRecord(f.done, stream), "record the call's completion");
-  f.stream = stream;
-  f.pending = true;
   return EBAG_OK;
 }
 
