@@ -130,6 +130,73 @@ int gemv_ar_launch_info(gemv_ar_t h, int32_t out[5]);
 /* Release the plan's device memory.  NULL is ignored. */
 void gemv_ar_destroy(gemv_ar_t h);
 
+/*
+ * Products with 4-bit weights and group scales.
+ *
+ * E matrices of M x K weights (E = experts; 1 for a plain layer) in 4 bits:
+ *
+ *   W[e][m][k] = scales[e][m][k / group] * (code[e][m][k] - zeros[e][m][k / group])
+ *
+ *   codes   uint8 [E][M][ceil(K / 2)]: column k in the low (k even) or high (k
+ *           odd) four bits of byte k / 2 of its row
+ *   scales  [E][M][ceil(K / group)] of the plan's type dtype
+ *   zeros   uint8 of the same shape, values 0..15; NULL: 8 everywhere
+ *
+ * group is a multiple of 32; the last group of a row may be short, K and M may
+ * be odd.  All three arrays are contiguous; codes are read in 16-byte vectors at
+ * any address (rows of a multiple of 32 columns on a 16-byte boundary are the
+ * fastest).
+ *
+ *   forward: y[n][m] = sum_k W[0][m][k] x[n][k],            n < rows
+ *   experts: y[p][m] = sum_k W[e][m][k] xrow(p)[k],          offsets[e] <= p < offsets[e + 1]
+ *
+ * With glu = 1 the M rows are M / 2 gate rows and M / 2 up rows and the result
+ * has M / 2 columns, y = silu(gate) * up, silu(v) = v / (1 + exp(-v)).
+ *
+ * x rows are K elements of dtype (EBAG_F32, EBAG_F16 or EBAG_BF16), row r at
+ * element r * ldx; y rows are of dtype or fp32 (y_dtype), row r at element
+ * r * ldy; neither needs an alignment beyond its elements'.  Sums are fp32,
+ * fp32 x counts with all its 24 bits, and a result is rounded once.  |x| * 31
+ * summed over a group must stay finite in fp32.  A row of x with an infinity or
+ * NaN gives infinities or NaN in its own row of y only.  Outputs must not
+ * overlap inputs.  Results do not depend on the other rows' values and are the
+ * same bits on every run.
+ */
+typedef struct gemv_ar_q4_plan* gemv_ar_q4_t;
+
+/* Create a plan on the current HIP device for E = experts (1..512) matrices
+ * of M rows and K columns (M * K below 2^40, both below 2^31), group a positive
+ * multiple of 32, glu 0 or 1 (M even).  It owns no device memory; its calls
+ * share nothing, may run on any stream and can be captured into a graph.  They
+ * must be made with the plan's device current (EBAG_EINVAL otherwise). */
+int gemv_ar_q4_create(gemv_ar_q4_t* out, int64_t M, int64_t K, int32_t group, int32_t dtype, int32_t experts,
+                      int32_t glu);
+
+/* Round weights w [E][M][K] (contiguous, of dtype, finite) to 4 bits.  With
+ * zeros, a group's scale is (max(w, 0) - min(w, 0)) / 15 and its zero the code
+ * of 0; without, the scale is max|w| / 7 and the zero 8.  The scale is rounded
+ * to dtype first and a code is the nearest to w / scale (halves to even) from
+ * that zero on, kept in 0..15; a scale of 0 gives the zero's code. */
+int gemv_ar_q4_quantize(gemv_ar_q4_t h, const void* w, uint8_t* codes, void* scales, uint8_t* zeros,
+                        hipStream_t stream);
+
+/* x [rows][K] times the (first) matrix: y [rows][M, or M / 2 with glu]. */
+int gemv_ar_q4_forward(gemv_ar_q4_t h, const uint8_t* codes, const void* scales, const uint8_t* zeros, const void* x,
+                       int64_t ldx, int64_t rows, void* y, int64_t ldy, int32_t y_dtype, hipStream_t stream);
+
+/* Every expert's rows times its matrix.  offsets: device int32 [E + 1], as
+ * the sort of ebag_a2a_moe_sort gives them; rows p from offsets[E] on (dropped
+ * choices) get zeros.  src NULL: xrow(p) is row p of x, which has x_rows =
+ * rows rows; otherwise xrow(p) is row src[p] / choices of x, whose x_rows are the
+ * tokens' own (src of the sort: no dispatch is needed).  Offsets and rows out of
+ * range are clamped into it. */
+int gemv_ar_q4_experts(gemv_ar_q4_t h, const uint8_t* codes, const void* scales, const uint8_t* zeros, const void* x,
+                       int64_t ldx, int64_t x_rows, const int32_t* offsets, const int32_t* src, int32_t choices,
+                       int64_t rows, void* y, int64_t ldy, int32_t y_dtype, hipStream_t stream);
+
+/* Release the plan.  NULL is ignored. */
+void gemv_ar_q4_destroy(gemv_ar_q4_t h);
+
 #ifdef __cplusplus
 }
 #endif

@@ -104,6 +104,14 @@ _SIGS = {
     "gemv_ar_reset": ([_P], ctypes.c_int),
     "gemv_ar_launch_info": ([_P, _P], ctypes.c_int),
     "gemv_ar_destroy": ([_P], None),
+    "gemv_ar_q4_create": ([_P, ctypes.c_int64, ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
+                           ctypes.c_int32], ctypes.c_int),
+    "gemv_ar_q4_quantize": ([_P, _P, _P, _P, _P, _P], ctypes.c_int),
+    "gemv_ar_q4_forward": ([_P, _P, _P, _P, _P, ctypes.c_int64, ctypes.c_int64, _P, ctypes.c_int64, ctypes.c_int32, _P],
+                           ctypes.c_int),
+    "gemv_ar_q4_experts": ([_P, _P, _P, _P, _P, ctypes.c_int64, ctypes.c_int64, _P, _P, ctypes.c_int32, ctypes.c_int64,
+                            _P, ctypes.c_int64, ctypes.c_int32, _P], ctypes.c_int),
+    "gemv_ar_q4_destroy": ([_P], None),
 }
 
 
@@ -584,6 +592,82 @@ class GemvAR:
     def close(self):
         if getattr(self, "_h", None):
             self._lib.gemv_ar_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class Q4Gemv:
+    """A plan for products with 4-bit weights and group scales
+    (``gemv_ar_q4_create``): `experts` matrices of M rows and K columns, a scale
+    for every `group` columns, storage type dtype; glu=1: y = silu(gate) * up of
+    the two halves of the M rows.  Methods mirror the C ABI and take torch tensors:
+    codes uint8 [experts, M, ceil(K / 2)], scales [experts, M, ceil(K / group)],
+    zeros uint8 of that shape or None, x and y with any step between rows, y of
+    the plan's type or float32."""
+
+    def __init__(self, M: int, K: int, group: int, dtype: int, experts: int = 1, glu: int = 0):
+        lib = load()
+        h = ctypes.c_void_p()
+        _check(lib.gemv_ar_q4_create(ctypes.byref(h), int(M), int(K), int(group), int(dtype), int(experts), int(glu)))
+        self._h = h
+        self._lib = lib
+        self._shape(M, K, group, dtype, experts, glu)
+
+    def _shape(self, M, K, group, dtype, experts, glu):
+        self.M, self.K, self.group, self.matrices = int(M), int(K), int(group), int(experts)
+        self.wide = self.M // 2 if glu else self.M
+        self.kind = {v: n for n, v in ROW_TYPES.items()}[int(dtype)]
+        self._rows = self.matrices * self.M
+
+    def _weights(self, codes, scales, zeros):
+        groups = -(-self.K // self.group)
+        _need(codes, self._rows * ((self.K + 1) // 2), "codes")
+        _need(scales, self._rows * groups * (4 if self.kind == "float32" else 2), "scales")
+        _need(zeros, self._rows * groups, "zeros")
+        _validate(((codes,), "codes", ("uint8",), None), ((scales,), "scales", (self.kind,), None),
+                  ((zeros,), "zeros", ("uint8",), None))
+
+    def quantize(self, w, codes, scales, zeros=None, stream=None):
+        self._weights(codes, scales, zeros)
+        _need(w, self._rows * self.K * (4 if self.kind == "float32" else 2), "w")
+        _validate(((w,), "w", (self.kind,), None))
+        _check(self._lib.gemv_ar_q4_quantize(self._h, w.data_ptr(), codes.data_ptr(), scales.data_ptr(), _addr(zeros),
+                                             _stream(stream)))
+
+    def _y(self, y, rows):
+        kind = "float32" if _dtype_name(y.dtype) == "float32" else self.kind
+        py, ldy, _ = _matrix(y, rows, self.wide, kind, "y")
+        return py, ldy, ROW_TYPES[kind]
+
+    def forward(self, codes, scales, zeros, x, y, stream=None):
+        self._weights(codes, scales, zeros)
+        rows = x.shape[0]
+        px, ldx, _ = _matrix(x, rows, self.K, self.kind, "x")
+        py, ldy, y_type = self._y(y, rows)
+        _check(self._lib.gemv_ar_q4_forward(self._h, codes.data_ptr(), scales.data_ptr(), _addr(zeros), px, ldx, rows,
+                                            py, ldy, y_type, _stream(stream)))
+
+    def experts(self, codes, scales, zeros, x, offsets, y, src=None, k=1, stream=None):
+        """gemv_ar_q4_experts; k: choices of a token, which src counts in."""
+        self._weights(codes, scales, zeros)
+        _need(offsets, 4 * (self.matrices + 1), "offsets")
+        _validate(((offsets,), "offsets", I32, None), ((src,), "src", I32, None))
+        x_rows = x.shape[0]
+        rows = x_rows if src is None else src.numel()
+        px, ldx, _ = _matrix(x, x_rows, self.K, self.kind, "x")
+        py, ldy, y_type = self._y(y, rows)
+        _check(self._lib.gemv_ar_q4_experts(self._h, codes.data_ptr(), scales.data_ptr(), _addr(zeros), px, ldx, x_rows,
+                                            offsets.data_ptr(), _addr(src), int(k), rows, py, ldy, y_type,
+                                            _stream(stream)))
+
+    def close(self):
+        if getattr(self, "_h", None):
+            self._lib.gemv_ar_q4_destroy(self._h)
             self._h = None
 
     def __del__(self):
