@@ -30,28 +30,38 @@ struct Q4Args {
   int32_t y_f32;
   Divisor by_choices;
   Divisor by_group_blocks;  // group / 32
-  Divisor by_tiles;         // tiles of weight rows
+  Divisor by_tiles;         // workgroups that share the rows of x, each with its rows of weights
+  // The kernel for few rows.
+  int32_t split;            // waves that share a tile
+  int32_t turns;            // tiles that a wave works through
+  int32_t x_bytes;          // LDS for x; the waves' sums lie behind
+  int32_t all_columns;      // K in whole units
+  int32_t some_columns;     // columns of 16 rows of x that fit, in whole units for each of a tile's waves
+  int32_t fit_rows;         // rows of x that fit with all their columns
+  Divisor by_all, by_some;  // those columns / 8
 };
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
-// A weight's code q goes through the matrix instructions as 16 + q, which is a
-// bit pattern away in fp16 and bf16 (16 is 2^4: q fills the top of the
-// mantissa) and exact in both; the 16 and the zero point come off again as
-// (16 + zero) * (the sum of x over the group).  fp32 x goes as three bf16
-// parts whose sum is x, bit for bit, so its products are exact too.
+// A weight's code q goes through the matrix instructions as BASE + q, which is a
+// bit pattern away in fp16 and bf16 (BASE is a power of two with q at the bottom
+// of its mantissa, or above it) and exact; BASE and the zero point come off again
+// as (BASE + zero) * (the sum of x over the group).  The sums grow by BASE / 8 at
+// most that way, so fp32 loses 3 bits (fp16), 4 (bf16) or 1 (fp32) of its 24: the
+// larger BASE leaves one code of four where it is and saves its shift.  fp32 x
+// goes as three bf16 parts whose sum is x, bit for bit, so its products are exact
+// too.
 template <int DT> struct Q4Type;
 
 template <> struct Q4Type<1> {
   static constexpr int PARTS = 1;
   static constexpr uint32_t ONES = 0x3C003C00u;
-  // Codes j and j + 4 of a word of eight (low bits first), as 16 + q.
-  static __device__ __forceinline__ uint32_t pair(uint32_t w, int j) {
-    const uint32_t v = j == 0 ? w << 6 : j == 1 ? w << 2 : j == 2 ? w >> 2 : w >> 6;
-    return (v & 0x03C003C0u) | 0x4C004C00u;
-  }
+  static constexpr float BASE = 64.f;
+  static constexpr uint32_t MASK = 0x00F000F0u, HIGH = 0x54005400u;
+  // Codes j and j + 4 of a word of eight (low bits first), under MASK.
+  static __device__ __forceinline__ uint32_t pair(uint32_t w, int j) { return j == 0 ? w << 4 : w >> (4 * (j - 1)); }
   static __device__ __forceinline__ f32x4 mfma(const vec16& a, const vec16& b, const f32x4& c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
   }
@@ -60,10 +70,9 @@ template <> struct Q4Type<1> {
 template <> struct Q4Type<2> {
   static constexpr int PARTS = 1;
   static constexpr uint32_t ONES = 0x3F803F80u;
-  static __device__ __forceinline__ uint32_t pair(uint32_t w, int j) {
-    const uint32_t v = j == 0 ? w << 3 : j == 1 ? w >> 1 : j == 2 ? w >> 5 : w >> 9;
-    return (v & 0x00780078u) | 0x41804180u;
-  }
+  static constexpr float BASE = 128.f;
+  static constexpr uint32_t MASK = 0x000F000Fu, HIGH = 0x43004300u;
+  static __device__ __forceinline__ uint32_t pair(uint32_t w, int j) { return w >> (4 * j); }
   static __device__ __forceinline__ f32x4 mfma(const vec16& a, const vec16& b, const f32x4& c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
   }
@@ -71,14 +80,28 @@ template <> struct Q4Type<2> {
 
 template <> struct Q4Type<0> : Q4Type<2> {
   static constexpr int PARTS = 3;
+  static constexpr float BASE = 16.f;
+  static constexpr uint32_t MASK = 0x00780078u, HIGH = 0x41804180u;
+  static __device__ __forceinline__ uint32_t pair(uint32_t w, int j) { return j == 0 ? w << 3 : w >> (4 * j - 3); }
 };
 
-// Eight codes of a word in the order of pair(): 0 4, 1 5, 2 6, 3 7.
+// MASK and HIGH in registers: as literals they would take an instruction each,
+// and from one scalar and one vector register both go into one.
 template <int DT>
-__device__ __forceinline__ vec16 unpack_codes(uint32_t w) {
+struct CodeBits {
+  uint32_t mask, high;
+  __device__ __forceinline__ CodeBits() {
+    asm volatile("s_mov_b32 %0, %1" : "=s"(mask) : "i"(Q4Type<DT>::MASK));
+    asm volatile("v_mov_b32 %0, %1" : "=v"(high) : "i"(Q4Type<DT>::HIGH));
+  }
+};
+
+// Eight codes of a word as BASE + q, in the order 0 4, 1 5, 2 6, 3 7.
+template <int DT>
+__device__ __forceinline__ vec16 unpack_codes(const CodeBits<DT>& c, uint32_t w) {
   vec16 r;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) r[j] = Q4Type<DT>::pair(w, j);
+  for (int j = 0; j < 4; ++j) r[j] = (Q4Type<DT>::pair(w, j) & c.mask) | c.high;
   return r;
 }
 
@@ -110,6 +133,37 @@ __device__ __forceinline__ void split_f32(const vec16& lo, const vec16& hi, vec1
   for (int p = 0; p < 3; ++p)
 #pragma unroll
     for (int j = 0; j < 4; ++j) parts[p][j] = __builtin_amdgcn_perm(cut[p][j + 4], cut[p][j], 0x07060302u);
+}
+
+// 16 bytes of codes; what lies behind a row's end is not used, what lies
+// behind the last matrix is not read.
+__device__ __forceinline__ vec16 load_codes_end(const Q4Args& a, const uint8_t* p) {
+  if (p + 16 <= a.codes + a.codes_bytes) return load16(reinterpret_cast<const char*>(p));
+  vec16 r = {0, 0, 0, 0};
+  for (int i = 0; i < 16; ++i)
+    if (p + i < a.codes + a.codes_bytes) r[i / 4] |= (uint32_t)p[i] << (8 * (i % 4));
+  return r;
+}
+
+// The first n of eight elements of x, zeros behind them.
+template <int DT>
+__device__ __forceinline__ void load_x(const char* p, int n, vec16* v) {
+  constexpr int VECS = DT == 0 ? 2 : 1;
+  if (n >= 8) {
+#pragma unroll
+    for (int i = 0; i < VECS; ++i) v[i] = load16(p + 16 * i);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < VECS; ++i) v[i] = vec16{0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    if (i >= n) continue;
+    if (DT == 0)
+      v[i / 4][i % 4] = reinterpret_cast<const uint32_t*>(p)[i];
+    else
+      v[0][i / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[i] << (16 * (i % 2));
+  }
 }
 
 // Which rows of y, and whose matrix, slot number `slot` of tiles of `cols` rows
@@ -167,5 +221,11 @@ __device__ __forceinline__ void store_y(const Q4Args& a, uint32_t n, int64_t m, 
 }
 
 __device__ __forceinline__ float silu(float v) { return v / (1.f + __expf(-v)); }
+
+// The matrix-product kernel for many rows of fp16 or bf16 x: a workgroup for
+// kQ4TileRows rows of weights (half as many outputs with glu) and 32 x_tiles (1 or
+// 2) rows of x.
+constexpr int kQ4TileRows = 256;
+void launch_q4_tile(const Q4Args& a, int dtype, int x_tiles, unsigned grid, hipStream_t stream);
 
 }  // namespace ebag

@@ -1,0 +1,269 @@
+// Products with 4-bit weights for many rows of x: the matrix-product kernel.
+#include <hip/hip_runtime.h>
+
+#include "gemv_ar.h"
+#include "q4.h"
+
+namespace ebag {
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kStep = 128;   // columns of a step
+constexpr int kB = 2;        // a wave's tiles of 32 weight rows
+
+template <int DT>
+__device__ __forceinline__ f32x16 mfma32(const vec16& a, const vec16& b, const f32x16& c) {
+  if (DT == 1)
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// Sum of the eight elements of a vector.
+template <int DT>
+__device__ __forceinline__ float sum8(const vec16& v) {
+  float f[8];
+  Type<DT>::widen(v, f);
+  return ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
+}
+
+// A float as the first three elements of a vector, exactly: three bf16 (8 bits
+// each), or three fp16 (11 bits each).
+template <int DT>
+__device__ __forceinline__ vec16 three_parts(float f) {
+  uint32_t p[3];
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    const typename Type<DT>::elt e = Type<DT>::narrow(f);
+    p[i] = __builtin_bit_cast(uint16_t, e);
+    f -= Type<DT>::widen(e);
+  }
+  return vec16{p[0] | p[1] << 16, p[2], 0, 0};
+}
+
+// WHOLE: a group is a multiple of 128 columns, so a step has one scale; otherwise
+// every block of 32 columns has its own.
+template <int DT, int NT, bool WHOLE>
+struct Tile {
+  static constexpr int BN = 32 * NT;                  // rows of x
+  static constexpr int GROUPS = WHOLE ? 1 : 4;        // of a step
+  static constexpr int PITCH = WHOLE ? 272 : 336;     // bytes of a row of x in LDS: 16 lanes' vectors on different banks
+  static constexpr int STAGED = BN * 16 / kThreads;   // vectors of a thread
+};
+
+// A workgroup has 256 rows of weights and BN = 32 NT rows of x, a wave 64 of the
+// weight rows and all rows of x.  x goes through LDS, two steps of 128 columns in
+// turn; a wave's codes come straight from memory, a step ahead, are made 16-bit
+// numbers BASE + q in registers and are multiplied from there, so every weight is
+// unpacked once for BN rows.  A group's sums start at zero, are corrected for BASE
+// and the zero point, and are added to the tile's sums times the scale.  The
+// correction, -(BASE + zero) * (sum of x), is one more matrix instruction: the
+// sum of x is found when x is staged and lies behind its row in three parts, whose
+// sum is exact, and the other operand is -(BASE + zero) three times.
+template <int DT, int NT, bool WHOLE>
+__global__ __launch_bounds__(kThreads, 1) void q4_tile_kernel(const Q4Args a) {
+  typedef Tile<DT, NT, WHOLE> C;
+  typedef Type<DT> T;
+  typedef Q4Type<DT> Q;
+  __shared__ __attribute__((aligned(16))) char lds[2][C::BN * C::PITCH];
+  const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, r32 = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const uint32_t slot = divide_by(a.by_tiles, blockIdx.x);
+  int expert;
+  uint32_t first, end;
+  if (!find_tile(a, slot, C::BN, &expert, &first, &end)) return;
+  // Rows of weights: with glu, a wave's two tiles are gate rows and the up rows that go with them.
+  const int pair = a.glu ? 2 : 1;
+  const int64_t wg_m0 = (int64_t)(blockIdx.x - slot * a.by_tiles.d) * (32 * kB * kWaves / pair);
+  if (expert == a.experts) {
+    const uint32_t cols = 32 * kB * kWaves / pair;
+    for (uint32_t i = tid; i < C::BN * cols; i += kThreads) {
+      const uint32_t n = first + i / cols;
+      const int64_t m = wg_m0 + i % cols;
+      if (n < end && m < a.out_rows) store_y<DT>(a, n, m, 0.f);
+    }
+    return;
+  }
+  const int64_t m0 = wg_m0 + wave * (32 * kB / pair);
+  const uint8_t* codes[kB];
+  const typename T::elt* scales[kB];
+  const uint8_t* zeros[kB];
+#pragma unroll
+  for (int b = 0; b < kB; ++b) {
+    int64_t m = m0 + (pair == 2 ? 0 : 32 * b) + r32;
+    m = m < a.out_rows ? m : a.out_rows - 1;
+    if (pair == 2 && b) m += a.out_rows;
+    m += (int64_t)expert * a.M;
+    codes[b] = a.codes + m * a.row_bytes + half * 16;
+    scales[b] = reinterpret_cast<const typename T::elt*>(a.scales) + m * a.groups;
+    zeros[b] = a.zeros ? a.zeros + m * a.groups : a.codes;
+  }
+  // Staging: thread (row, chunk) has vector `chunk` of rows row, row + 16, ...
+  const int chunk = tid & 15;
+  const char* x[C::STAGED];
+#pragma unroll
+  for (int i = 0; i < C::STAGED; ++i) {
+    uint32_t n = first + (tid >> 4) + 16 * i;
+    n = n < end ? n : end - 1;
+    int64_t row = a.src ? (int64_t)divide_by(a.by_choices, (uint32_t)a.src[n] & 0x7fffffffu) : (int64_t)n;
+    row = row < a.x_rows ? row : a.x_rows - 1;
+    x[i] = a.x + row * a.ldx + chunk * 16;
+  }
+
+  struct Weights {
+    vec16 w[kB][2];  // bytes half * 16 .. of each 32: word j has columns 64 i + 32 half + 8 j
+    typename T::elt scale[kB][C::GROUPS];
+    uint32_t zero[kB][C::GROUPS];
+  };
+  auto load_weights = [&](Weights& o, int step) {
+    const bool whole = (step + 1) * kStep <= a.K;
+#pragma unroll
+    for (int b = 0; b < kB; ++b)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint8_t* p = codes[b] + (int64_t)step * (kStep / 2) + 32 * i;
+        o.w[b][i] = whole ? load16(reinterpret_cast<const char*>(p)) : load_codes_end(a, p);
+      }
+#pragma unroll
+    for (int g = 0; g < C::GROUPS; ++g) {
+      uint32_t at = divide_by(a.by_group_blocks, (uint32_t)(step * 4 + g));
+      at = at < (uint32_t)a.groups ? at : a.groups - 1;
+#pragma unroll
+      for (int b = 0; b < kB; ++b) {
+        o.scale[b][g] = scales[b][at];
+        const uint32_t z = zeros[b][a.zeros ? at : 0u];
+        o.zero[b][g] = a.zeros ? z : 8u;
+      }
+    }
+  };
+  auto load_rows = [&](vec16* v, int step) {
+    const int n = a.K - step * kStep - 8 * chunk;  // elements left
+#pragma unroll
+    for (int i = 0; i < C::STAGED; ++i) load_x<DT>(x[i] + (int64_t)step * (kStep * 2), n, &v[i]);
+  };
+  auto store_rows = [&](const vec16* v, char* to) {
+#pragma unroll
+    for (int i = 0; i < C::STAGED; ++i) {
+      char* row = to + ((tid >> 4) + 16 * i) * C::PITCH;
+      float s = sum8<DT>(v[i]);
+#pragma unroll
+      for (int d = 1; d < (WHOLE ? 16 : 4); d *= 2) s += __shfl_xor(s, d);
+      *reinterpret_cast<vec16*>(row + chunk * 16) = pair_order(v[i]);
+      if ((chunk & (WHOLE ? 15 : 3)) == 0) *reinterpret_cast<vec16*>(row + 256 + chunk * 4) = three_parts<DT>(s);
+    }
+  };
+
+  const CodeBits<DT> bits;
+  f32x16 sum[kB][NT];
+#pragma unroll
+  for (int b = 0; b < kB; ++b)
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sum[b][t][i] = 0.f;
+
+  const int steps = (a.K + kStep - 1) / kStep;
+  Weights now, next;
+  vec16 staged[C::STAGED];
+  load_rows(staged, 0);
+  load_weights(now, 0);
+  store_rows(staged, lds[0]);
+  __syncthreads();
+  for (int step = 0; step < steps; ++step) {
+    const bool more = step + 1 < steps;
+    if (more) {
+      load_weights(next, step + 1);
+      load_rows(staged, step + 1);
+    }
+    const char* from = lds[step & 1] + r32 * C::PITCH;
+#pragma unroll
+    for (int b = 0; b < kB; ++b)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; j += 2) {  // columns 8 half .. of 16 in both halves
+          const u32x2 s = __builtin_amdgcn_permlane32_swap(now.w[b][i][j], now.w[b][i][j + 1], false, false);
+          now.w[b][i][j] = s[0];
+          now.w[b][i][j + 1] = s[1];
+        }
+#pragma unroll
+    for (int g = 0; g < C::GROUPS; ++g) {
+      f32x16 v[kB][NT];
+#pragma unroll
+      for (int sl = 0; sl < 9 - C::GROUPS - (C::GROUPS == 4 ? 2 : 0); ++sl) {
+        if (WHOLE ? sl < 8 : sl < 2) {
+          const int slice = WHOLE ? sl : 2 * g + sl;  // of 16 columns
+          vec16 xs[NT];
+#pragma unroll
+          for (int t = 0; t < NT; ++t) xs[t] = *reinterpret_cast<const vec16*>(from + 32 * t * C::PITCH + slice * 32 + half * 16);
+#pragma unroll
+          for (int b = 0; b < kB; ++b) {
+            // Of each 64 columns: words 0, 2 have the first 32, words 1, 3 the others.
+            const vec16 q = unpack_codes(bits, now.w[b][slice / 4][slice % 4 / 2 + 2 * (slice % 2)]);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+              if (sl == 0)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) v[b][t][i] = 0.f;
+              v[b][t] = mfma32<DT>(xs[t], q, v[b][t]);
+            }
+          }
+        }
+      }
+      vec16 xsum[NT];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) xsum[t] = *reinterpret_cast<const vec16*>(from + 32 * t * C::PITCH + 256 + g * 16);
+#pragma unroll
+      for (int b = 0; b < kB; ++b) {
+        const uint32_t o = __builtin_bit_cast(uint16_t, T::narrow(-Q::BASE - (float)now.zero[b][g]));
+        const vec16 off = {half ? 0u : o | o << 16, half ? 0u : o, 0, 0};
+        const float scale = T::widen(now.scale[b][g]);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          v[b][t] = mfma32<DT>(xsum[t], off, v[b][t]);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) sum[b][t][i] = __builtin_fmaf(scale, v[b][t][i], sum[b][t][i]);
+        }
+      }
+    }
+    if (more) {
+      store_rows(staged, lds[(step + 1) & 1]);
+      now = next;
+    }
+    __syncthreads();
+  }
+  // A lane has weight row r32 and, in element i, row 8 (i / 4) + 4 half + i % 4 of x.
+#pragma unroll
+  for (int b = 0; b < kB; ++b) {
+    if (pair == 2 && b) continue;
+    const int64_t m = m0 + 32 * b + r32;
+    if (m >= a.out_rows) continue;
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const uint32_t n = first + 32 * t + 8 * (i / 4) + 4 * half + i % 4;
+        if (n < end) store_y<DT>(a, n, m, pair == 2 ? silu(sum[0][t][i]) * sum[1][t][i] : sum[b][t][i]);
+      }
+  }
+}
+
+typedef void (*tile_fn)(const Q4Args);
+
+template <int NT>
+tile_fn pick(int dt, bool whole) {
+  return dt == EBAG_F16 ? (whole ? q4_tile_kernel<1, NT, true> : q4_tile_kernel<1, NT, false>)
+                        : (whole ? q4_tile_kernel<2, NT, true> : q4_tile_kernel<2, NT, false>);
+}
+
+}  // namespace
+
+void launch_q4_tile(const Q4Args& a, int dtype, int x_tiles, unsigned grid, hipStream_t stream) {
+  const bool whole = a.group % 128 == 0;
+  const tile_fn fn = x_tiles == 1 ? pick<1>(dtype, whole) : pick<2>(dtype, whole);
+  hipLaunchKernelGGL(fn, dim3(grid), dim3(kThreads), 0, stream, a);
+}
+
+}  // namespace ebag

@@ -21,6 +21,10 @@ __device__ __forceinline__ void store16(char* p, const vec16& v) { *reinterpret_
 // rounded to nearest even.
 template <int DT> struct Type;
 
+// Its elements' bits.
+template <int DT> struct Bits { typedef uint16_t type; };
+template <> struct Bits<0> { typedef uint32_t type; };
+
 template <> struct Type<0> {
   typedef float elt;
   static constexpr int N = 4;  // elements of a vector
