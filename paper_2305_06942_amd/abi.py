@@ -152,10 +152,28 @@ def _addr(x) -> Optional[int]:
     return x.data_ptr()
 
 
+_current_stream = None  # the current device's current stream, as an address
+
+
+def _find_current_stream():
+    """torch.cuda.current_stream() builds a stream object, 2.9 us of a call
+    that takes 6 in all; torch also has the stream's address alone."""
+    import torch
+    raw, device = (getattr(torch._C, n, None) for n in ("_cuda_getCurrentRawStream", "_cuda_getDevice"))
+    if raw is None or device is None:
+        return lambda: torch.cuda.current_stream().cuda_stream
+    return lambda: raw(device())
+
+
 def _stream(stream) -> Optional[int]:
+    global _current_stream
     if stream is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+        if _current_stream is None:
+            import torch
+            if not torch.cuda.is_initialized():
+                return torch.cuda.current_stream().cuda_stream
+            _current_stream = _find_current_stream()
+        return _current_stream()
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -416,20 +434,38 @@ class Plan:
 ROW_TYPES = {"float32": EBAG_F32, "float16": EBAG_F16, "bfloat16": EBAG_BF16}
 
 
+def _refuse(*specs):
+    """Says what is wrong with tensors that _fit() turned down.  specs: (tensor,
+    name, allowed dtype names, bytes needed)."""
+    _validate(*(((x,), what, kinds, None) for x, what, kinds, _ in specs))
+    for x, what, _, nbytes in specs:
+        _need(x, nbytes, what)
+    raise ValueError(f"unusable tensors among {', '.join(what for _, what, _, _ in specs)}")
+
+
+def _fit(x, dtype, count: int) -> bool:
+    """Whether a tensor is one of at least `count` elements that a kernel can
+    take: _validate() and _need() in one go, for calls of a few microseconds."""
+    return x.dtype is dtype and x.is_cuda and x.is_contiguous() and x.numel() >= count
+
+
 def _matrix(x, rows: int, cols: int, kind: Optional[str], what: str):
     """(address, row step in elements, type name) of a matrix on the GPU: a
     tensor [rows or more, cols] whose rows are contiguous, one step apart."""
-    name = _dtype_name(x.dtype)
+    name = _DTYPES.get(x.dtype) or _dtype_name(x.dtype)
     if name not in ROW_TYPES or (kind is not None and name != kind):
         raise ValueError(f"{what} must be {kind or ' or '.join(ROW_TYPES)}, not {name}")
-    if x.dim() != 2 or x.shape[0] < rows or x.shape[1] != cols:
-        raise ValueError(f"{what} must be [{rows}, {cols}], not {list(x.shape)}")
-    inner, step = x.stride(1), x.stride(0)
-    if (inner != 1 and cols > 1) or (step < cols and x.shape[0] > 1):
+    shape = x.shape
+    if len(shape) != 2 or shape[0] < rows or shape[1] != cols:
+        raise ValueError(f"{what} must be [{rows}, {cols}], not {list(shape)}")
+    step, inner = x.stride()
+    if shape[0] <= 1:
+        step = cols
+    if (inner != 1 and cols > 1) or step < cols:
         raise ValueError(f"{what} must have contiguous rows that do not overlap")
     if not x.is_cuda:
         raise ValueError(f"{what} must be a GPU tensor, not one on {x.device}")
-    return x.data_ptr(), (step if x.shape[0] > 1 else cols), name
+    return x.data_ptr(), step, name
 
 
 class MoePerm:
@@ -446,29 +482,35 @@ class MoePerm:
         _check(lib.ebag_a2a_moe_create(ctypes.byref(h), int(max_tokens), int(choices), int(experts)))
         self._h = h
         self._lib = lib
-        self.choices, self.experts = int(choices), int(experts)
+        self._shape(choices, experts)
 
-    def _places(self, offsets, pos, weights=None, dweights=None) -> int:
-        """Checks what every call over rows shares; the number of tokens."""
-        _validate(((offsets,), "offsets", I32, None), ((pos,), "pos", I32, None), ((weights,), "weights", F32, None),
-                  ((dweights,), "dweights", F32, None))
-        tokens = pos.numel() // self.choices
-        if pos.numel() != tokens * self.choices:
+    def _shape(self, choices, experts):
+        import torch
+        self.choices, self.experts = int(choices), int(experts)
+        self._i32, self._f32 = torch.int32, torch.float32
+
+    def _places(self, offsets, pos, *weights) -> int:
+        """Checks what every call over rows shares; the number of tokens.
+        weights: the call's float32 [tokens, choices] tensors."""
+        n = pos.numel()
+        tokens = n // self.choices
+        if n != tokens * self.choices:
             raise ValueError(f"pos must be [tokens, {self.choices}], not {list(pos.shape)}")
-        _need(offsets, 4 * (self.experts + 1), "offsets")
-        _need(weights, 4 * pos.numel(), "weights")
-        _need(dweights, 4 * pos.numel(), "dweights")
+        ok = _fit(offsets, self._i32, self.experts + 1) and _fit(pos, self._i32, 0)
+        for w in weights:
+            ok = ok and _fit(w, self._f32, n)
+        if not ok:
+            _refuse((offsets, "offsets", I32, 4 * (self.experts + 1)), (pos, "pos", I32, 0),
+                    *((w, what, F32, 4 * n) for w, what in zip(weights, ("weights", "dweights"))))
         return tokens
 
     def sort(self, experts_of, offsets, pos, src, stream=None):
-        _validate(((experts_of,), "experts_of", I32, None), ((offsets,), "offsets", I32, None),
-                  ((pos,), "pos", I32, None), ((src,), "src", I32, None))
-        n = experts_of.numel()
+        n, i32 = experts_of.numel(), self._i32
         if n % self.choices:
             raise ValueError(f"experts_of must be [tokens, {self.choices}], not {list(experts_of.shape)}")
-        _need(offsets, 4 * (self.experts + 1), "offsets")
-        _need(pos, 4 * n, "pos")
-        _need(src, 4 * n, "src")
+        if not (_fit(experts_of, i32, 0) and _fit(offsets, i32, self.experts + 1) and _fit(pos, i32, n) and _fit(src, i32, n)):
+            _refuse((experts_of, "experts_of", I32, 0), (offsets, "offsets", I32, 4 * (self.experts + 1)),
+                    (pos, "pos", I32, 4 * n), (src, "src", I32, 4 * n))
         _check(self._lib.ebag_a2a_moe_sort(self._h, experts_of.data_ptr(), n // self.choices, offsets.data_ptr(),
                                            pos.data_ptr(), src.data_ptr(), _stream(stream)))
 
@@ -622,25 +664,27 @@ class Q4Gemv:
         self.M, self.K, self.group, self.matrices = int(M), int(K), int(group), int(experts)
         self.wide = self.M // 2 if glu else self.M
         self.kind = {v: n for n, v in ROW_TYPES.items()}[int(dtype)]
-        self._rows = self.matrices * self.M
+        import torch
+        self._u8, self._i32, self._f32, self._dtype = torch.uint8, torch.int32, torch.float32, getattr(torch, self.kind)
+        rows = self.matrices * self.M
+        self._all, self._codes, self._groups = rows * self.K, rows * ((self.K + 1) // 2), rows * -(-self.K // self.group)
 
     def _weights(self, codes, scales, zeros):
-        groups = -(-self.K // self.group)
-        _need(codes, self._rows * ((self.K + 1) // 2), "codes")
-        _need(scales, self._rows * groups * (4 if self.kind == "float32" else 2), "scales")
-        _need(zeros, self._rows * groups, "zeros")
-        _validate(((codes,), "codes", ("uint8",), None), ((scales,), "scales", (self.kind,), None),
-                  ((zeros,), "zeros", ("uint8",), None))
+        if not (_fit(codes, self._u8, self._codes) and _fit(scales, self._dtype, self._groups) and
+                (zeros is None or _fit(zeros, self._u8, self._groups))):
+            _refuse((codes, "codes", ("uint8",), self._codes),
+                    (scales, "scales", (self.kind,), self._groups * self._dtype.itemsize),
+                    (zeros, "zeros", ("uint8",), self._groups))
 
     def quantize(self, w, codes, scales, zeros=None, stream=None):
         self._weights(codes, scales, zeros)
-        _need(w, self._rows * self.K * (4 if self.kind == "float32" else 2), "w")
-        _validate(((w,), "w", (self.kind,), None))
+        if not _fit(w, self._dtype, self._all):
+            _refuse((w, "w", (self.kind,), self._all * self._dtype.itemsize))
         _check(self._lib.gemv_ar_q4_quantize(self._h, w.data_ptr(), codes.data_ptr(), scales.data_ptr(), _addr(zeros),
                                              _stream(stream)))
 
     def _y(self, y, rows):
-        kind = "float32" if _dtype_name(y.dtype) == "float32" else self.kind
+        kind = self.kind if y.dtype is self._dtype or y.dtype is not self._f32 else "float32"
         py, ldy, _ = _matrix(y, rows, self.wide, kind, "y")
         return py, ldy, ROW_TYPES[kind]
 
@@ -655,8 +699,8 @@ class Q4Gemv:
     def experts(self, codes, scales, zeros, x, offsets, y, src=None, k=1, stream=None):
         """gemv_ar_q4_experts; k: choices of a token, which src counts in."""
         self._weights(codes, scales, zeros)
-        _need(offsets, 4 * (self.matrices + 1), "offsets")
-        _validate(((offsets,), "offsets", I32, None), ((src,), "src", I32, None))
+        if not (_fit(offsets, self._i32, self.matrices + 1) and (src is None or _fit(src, self._i32, 0))):
+            _refuse((offsets, "offsets", I32, 4 * (self.matrices + 1)), (src, "src", I32, 0))
         x_rows = x.shape[0]
         rows = x_rows if src is None else src.numel()
         px, ldx, _ = _matrix(x, x_rows, self.K, self.kind, "x")

@@ -24,9 +24,34 @@ __device__ __forceinline__ f32x16 mfma32(const vec16& a, const vec16& b, const f
 // Sum of the eight elements of a vector.
 template <int DT>
 __device__ __forceinline__ float sum8(const vec16& v) {
+  if (DT == 2) {
+    const bf16x2 ones = __builtin_bit_cast(bf16x2, 0x3F803F80u);
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t two = v[i];
+      s = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), ones, s, false);
+    }
+    return s;
+  }
   float f[8];
   Type<DT>::widen(v, f);
   return ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
+}
+
+template <int CTRL>
+__device__ __forceinline__ float add_lane(float v) {
+  return v + __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), CTRL, 0xf, 0xf, true));
+}
+
+// The sum over 4 or 16 neighbouring lanes, in each of them.
+template <int LANES>
+__device__ __forceinline__ float sum_lanes(float v) {
+  v = add_lane<0xB1>(v);   // quad_perm 1 0 3 2
+  v = add_lane<0x4E>(v);   // quad_perm 2 3 0 1
+  if (LANES == 4) return v;
+  v = add_lane<0x141>(v);  // row_half_mirror
+  return add_lane<0x140>(v);  // row_mirror
 }
 
 // A float as the first three elements of a vector, exactly: three bf16 (8 bits
@@ -62,21 +87,21 @@ struct Tile {
 // correction, -(BASE + zero) * (sum of x), is one more matrix instruction: the
 // sum of x is found when x is staged and lies behind its row in three parts, whose
 // sum is exact, and the other operand is -(BASE + zero) three times.
-template <int DT, int NT, bool WHOLE>
-__global__ __launch_bounds__(kThreads, 1) void q4_tile_kernel(const Q4Args a) {
+template <int DT, int NT, bool WHOLE, bool ZEROS>
+__global__ __launch_bounds__(kThreads, 2) void q4_tile_kernel(const Q4Args a) {
   typedef Tile<DT, NT, WHOLE> C;
   typedef Type<DT> T;
   typedef Q4Type<DT> Q;
   __shared__ __attribute__((aligned(16))) char lds[2][C::BN * C::PITCH];
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, r32 = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const uint32_t slot = divide_by(a.by_tiles, blockIdx.x);
+  const uint32_t slot = divide_by(a.by_tiles, blockIdx.x), tile = blockIdx.x - slot * a.by_tiles.d;
   int expert;
   uint32_t first, end;
   if (!find_tile(a, slot, C::BN, &expert, &first, &end)) return;
   // Rows of weights: with glu, a wave's two tiles are gate rows and the up rows that go with them.
   const int pair = a.glu ? 2 : 1;
-  const int64_t wg_m0 = (int64_t)(blockIdx.x - slot * a.by_tiles.d) * (32 * kB * kWaves / pair);
+  const int64_t wg_m0 = (int64_t)tile * (32 * kB * kWaves / pair);
   if (expert == a.experts) {
     const uint32_t cols = 32 * kB * kWaves / pair;
     for (uint32_t i = tid; i < C::BN * cols; i += kThreads) {
@@ -87,18 +112,23 @@ __global__ __launch_bounds__(kThreads, 1) void q4_tile_kernel(const Q4Args a) {
     return;
   }
   const int64_t m0 = wg_m0 + wave * (32 * kB / pair);
+  // Uniform addresses of the wave's first row of each tile, and a lane's 32-bit distances from them.
   const uint8_t* codes[kB];
-  const typename T::elt* scales[kB];
+  const char* scales[kB];
   const uint8_t* zeros[kB];
+  uint32_t codes_at[kB], group_at[kB];
 #pragma unroll
   for (int b = 0; b < kB; ++b) {
-    int64_t m = m0 + (pair == 2 ? 0 : 32 * b) + r32;
+    const int64_t from = m0 + (pair == 2 ? 0 : 32 * b);  // may lie behind the last row: then all lanes take that one
+    const int64_t base = from < a.out_rows ? from : a.out_rows - 1;
+    int64_t m = from + r32;
     m = m < a.out_rows ? m : a.out_rows - 1;
-    if (pair == 2 && b) m += a.out_rows;
-    m += (int64_t)expert * a.M;
-    codes[b] = a.codes + m * a.row_bytes + half * 16;
-    scales[b] = reinterpret_cast<const typename T::elt*>(a.scales) + m * a.groups;
-    zeros[b] = a.zeros ? a.zeros + m * a.groups : a.codes;
+    const int64_t row = base + (pair == 2 && b ? a.out_rows : 0) + (int64_t)expert * a.M;
+    codes[b] = a.codes + row * a.row_bytes;
+    scales[b] = a.scales + row * a.groups * 2;
+    zeros[b] = a.zeros ? a.zeros + row * a.groups : nullptr;
+    codes_at[b] = (uint32_t)(m - base) * (uint32_t)a.row_bytes + half * 16;
+    group_at[b] = (uint32_t)(m - base) * (uint32_t)a.groups;
   }
   // Staging: thread (row, chunk) has vector `chunk` of rows row, row + 16, ...
   const int chunk = tid & 15;
@@ -117,42 +147,49 @@ __global__ __launch_bounds__(kThreads, 1) void q4_tile_kernel(const Q4Args a) {
     typename T::elt scale[kB][C::GROUPS];
     uint32_t zero[kB][C::GROUPS];
   };
-  auto load_weights = [&](Weights& o, int step) {
-    const bool whole = (step + 1) * kStep <= a.K;
+  // tail: the step passes the end of K.
+  auto load_weights = [&](Weights& o, int step, bool tail) {
 #pragma unroll
     for (int b = 0; b < kB; ++b)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const uint8_t* p = codes[b] + (int64_t)step * (kStep / 2) + 32 * i;
-        o.w[b][i] = whole ? load16(reinterpret_cast<const char*>(p)) : load_codes_end(a, p);
+        const uint8_t* base = codes[b] + (int64_t)step * (kStep / 2) + 32 * i;
+        o.w[b][i] = tail ? load_codes_end(a, base + codes_at[b]) : load16(reinterpret_cast<const char*>(base) + codes_at[b]);
       }
 #pragma unroll
     for (int g = 0; g < C::GROUPS; ++g) {
       uint32_t at = divide_by(a.by_group_blocks, (uint32_t)(step * 4 + g));
-      at = at < (uint32_t)a.groups ? at : a.groups - 1;
+      if (tail) at = at < (uint32_t)a.groups ? at : a.groups - 1;
 #pragma unroll
       for (int b = 0; b < kB; ++b) {
-        o.scale[b][g] = scales[b][at];
-        const uint32_t z = zeros[b][a.zeros ? at : 0u];
-        o.zero[b][g] = a.zeros ? z : 8u;
+        o.scale[b][g] = *reinterpret_cast<const typename T::elt*>(scales[b] + 2 * at + 2 * group_at[b]);
+        o.zero[b][g] = ZEROS ? *(zeros[b] + at + group_at[b]) : 8u;
       }
     }
   };
-  auto load_rows = [&](vec16* v, int step) {
+  auto load_rows = [&](vec16* v, int step, bool tail) {
+    if (!tail) {
+#pragma unroll
+      for (int i = 0; i < C::STAGED; ++i) v[i] = load16(x[i] + (int64_t)step * (kStep * 2));
+      return;
+    }
     const int n = a.K - step * kStep - 8 * chunk;  // elements left
 #pragma unroll
     for (int i = 0; i < C::STAGED; ++i) load_x<DT>(x[i] + (int64_t)step * (kStep * 2), n, &v[i]);
   };
   auto store_rows = [&](const vec16* v, char* to) {
+    // Lane `chunk` of a row (or of a quarter of it) finishes the sums of row number `chunk` % STAGED.
+    float mine = 0.f;
+    const int pick = (WHOLE ? chunk : chunk & 3) % C::STAGED;
+    char* row = to + (tid >> 4) * C::PITCH;
 #pragma unroll
     for (int i = 0; i < C::STAGED; ++i) {
-      char* row = to + ((tid >> 4) + 16 * i) * C::PITCH;
-      float s = sum8<DT>(v[i]);
-#pragma unroll
-      for (int d = 1; d < (WHOLE ? 16 : 4); d *= 2) s += __shfl_xor(s, d);
-      *reinterpret_cast<vec16*>(row + chunk * 16) = pair_order(v[i]);
-      if ((chunk & (WHOLE ? 15 : 3)) == 0) *reinterpret_cast<vec16*>(row + 256 + chunk * 4) = three_parts<DT>(s);
+      const float s = sum_lanes<WHOLE ? 16 : 4>(sum8<DT>(v[i]));
+      mine = i == pick ? s : mine;
+      *reinterpret_cast<vec16*>(row + 16 * i * C::PITCH + chunk * 16) = pair_order(v[i]);
     }
+    if ((WHOLE ? chunk : chunk & 3) < C::STAGED)
+      *reinterpret_cast<vec16*>(row + 16 * pick * C::PITCH + 256 + (WHOLE ? 0 : chunk / 4 * 16)) = three_parts<DT>(mine);
   };
 
   const CodeBits<DT> bits;
@@ -164,18 +201,15 @@ __global__ __launch_bounds__(kThreads, 1) void q4_tile_kernel(const Q4Args a) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) sum[b][t][i] = 0.f;
 
-  const int steps = (a.K + kStep - 1) / kStep;
   Weights now, next;
   vec16 staged[C::STAGED];
-  load_rows(staged, 0);
-  load_weights(now, 0);
-  store_rows(staged, lds[0]);
-  __syncthreads();
-  for (int step = 0; step < steps; ++step) {
-    const bool more = step + 1 < steps;
-    if (more) {
-      load_weights(next, step + 1);
-      load_rows(staged, step + 1);
+  enum Next { WHOLE_STEP, TAIL_STEP, NONE };
+  // One step's products; what the next one needs is loaded ahead of them and staged behind.
+  auto work = [&](int step, Next after) __attribute__((always_inline)) {
+    if (after != NONE) {
+      load_weights(next, step + 1, after == TAIL_STEP);
+      load_rows(staged, step + 1, after == TAIL_STEP);
+
     }
     const char* from = lds[step & 1] + r32 * C::PITCH;
 #pragma unroll
@@ -188,27 +222,26 @@ __global__ __launch_bounds__(kThreads, 1) void q4_tile_kernel(const Q4Args a) {
           now.w[b][i][j] = s[0];
           now.w[b][i][j + 1] = s[1];
         }
+    constexpr int SLICES = 8 / C::GROUPS;  // of 16 columns, of a group
 #pragma unroll
     for (int g = 0; g < C::GROUPS; ++g) {
       f32x16 v[kB][NT];
 #pragma unroll
-      for (int sl = 0; sl < 9 - C::GROUPS - (C::GROUPS == 4 ? 2 : 0); ++sl) {
-        if (WHOLE ? sl < 8 : sl < 2) {
-          const int slice = WHOLE ? sl : 2 * g + sl;  // of 16 columns
-          vec16 xs[NT];
+      for (int sl = 0; sl < SLICES; ++sl) {
+        const int slice = g * SLICES + sl;
+        vec16 xs[NT];
 #pragma unroll
-          for (int t = 0; t < NT; ++t) xs[t] = *reinterpret_cast<const vec16*>(from + 32 * t * C::PITCH + slice * 32 + half * 16);
+        for (int t = 0; t < NT; ++t) xs[t] = *reinterpret_cast<const vec16*>(from + 32 * t * C::PITCH + slice * 32 + half * 16);
 #pragma unroll
-          for (int b = 0; b < kB; ++b) {
-            // Of each 64 columns: words 0, 2 have the first 32, words 1, 3 the others.
-            const vec16 q = unpack_codes(bits, now.w[b][slice / 4][slice % 4 / 2 + 2 * (slice % 2)]);
+        for (int b = 0; b < kB; ++b) {
+          // Of each 64 columns, words 0 and 2 have the first 32, words 1 and 3 the others.
+          const vec16 q = unpack_codes(bits, now.w[b][slice / 4][slice % 4 / 2 + 2 * (slice % 2)]);
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-              if (sl == 0)
+          for (int t = 0; t < NT; ++t) {
+            if (sl == 0)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) v[b][t][i] = 0.f;
-              v[b][t] = mfma32<DT>(xs[t], q, v[b][t]);
-            }
+              for (int i = 0; i < 16; ++i) v[b][t][i] = 0.f;
+            v[b][t] = mfma32<DT>(xs[t], q, v[b][t]);
           }
         }
       }
@@ -227,13 +260,23 @@ __global__ __launch_bounds__(kThreads, 1) void q4_tile_kernel(const Q4Args a) {
           for (int i = 0; i < 16; ++i) sum[b][t][i] = __builtin_fmaf(scale, v[b][t][i], sum[b][t][i]);
         }
       }
+      if (!WHOLE) __builtin_amdgcn_sched_barrier(0);  // one group's sums at a time: registers
     }
-    if (more) {
+    if (after != NONE) {
       store_rows(staged, lds[(step + 1) & 1]);
       now = next;
+      __syncthreads();
     }
-    __syncthreads();
-  }
+  };
+  const int whole = a.K / kStep, steps = (a.K + kStep - 1) / kStep;
+  load_rows(staged, 0, whole == 0);
+  load_weights(now, 0, whole == 0);
+  store_rows(staged, lds[0]);
+  __syncthreads();
+  int step = 0;
+  for (; step + 1 < whole; ++step) work(step, WHOLE_STEP);
+  if (step + 1 < steps) work(step++, TAIL_STEP);
+  work(step, NONE);
   // A lane has weight row r32 and, in element i, row 8 (i / 4) + 4 half + i % 4 of x.
 #pragma unroll
   for (int b = 0; b < kB; ++b) {
@@ -252,17 +295,18 @@ __global__ __launch_bounds__(kThreads, 1) void q4_tile_kernel(const Q4Args a) {
 
 typedef void (*tile_fn)(const Q4Args);
 
-template <int NT>
-tile_fn pick(int dt, bool whole) {
-  return dt == EBAG_F16 ? (whole ? q4_tile_kernel<1, NT, true> : q4_tile_kernel<1, NT, false>)
-                        : (whole ? q4_tile_kernel<2, NT, true> : q4_tile_kernel<2, NT, false>);
+template <int DT, int NT>
+tile_fn pick(bool whole, bool zeros) {
+  return whole ? (zeros ? q4_tile_kernel<DT, NT, true, true> : q4_tile_kernel<DT, NT, true, false>)
+               : (zeros ? q4_tile_kernel<DT, NT, false, true> : q4_tile_kernel<DT, NT, false, false>);
 }
 
 }  // namespace
 
 void launch_q4_tile(const Q4Args& a, int dtype, int x_tiles, unsigned grid, hipStream_t stream) {
   const bool whole = a.group % 128 == 0;
-  const tile_fn fn = x_tiles == 1 ? pick<1>(dtype, whole) : pick<2>(dtype, whole);
+  const tile_fn fn = dtype == EBAG_F16 ? (x_tiles == 1 ? pick<1, 1>(whole, a.zeros) : pick<1, 2>(whole, a.zeros))
+                                       : (x_tiles == 1 ? pick<2, 1>(whole, a.zeros) : pick<2, 2>(whole, a.zeros));
   hipLaunchKernelGGL(fn, dim3(grid), dim3(kThreads), 0, stream, a);
 }
 

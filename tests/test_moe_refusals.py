@@ -43,7 +43,8 @@ class _NoCalls:
 def _plan(choices=2, experts=4):
     import paper_2305_06942_amd as ebag
     p = object.__new__(ebag.MoePerm)
-    p._h, p._lib, p.choices, p.experts = None, _NoCalls(), choices, experts
+    p._h, p._lib = None, _NoCalls()
+    p._shape(choices, experts)
     return p
 
 
