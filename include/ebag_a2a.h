@@ -420,7 +420,7 @@ int ebag_a2a_moe_create(ebag_a2a_moe_t* out, int64_t max_tokens, int32_t choices
 
 /* Sort the choices: experts_of int32 [tokens][choices] -> offsets int32
  * [experts + 1], pos int32 [tokens][choices], src int32 [tokens * choices].
- * One launch up to 16384 choices, two above. */
+ * One launch up to 4096 choices, two above. */
 int ebag_a2a_moe_sort(ebag_a2a_moe_t h, const int32_t* experts_of, int64_t tokens, int32_t* offsets, int32_t* pos,
                       int32_t* src, hipStream_t stream);
 

@@ -334,3 +334,44 @@ def test_rows_on_a_stream_of_their_own():
     side.synchronize()
     assert bool((back == 6.0).all())
     plan.close()
+
+
+@pytest.mark.parametrize("N,k,D,dtype", [(9000, 8, 1024, "bfloat16"), (11000, 6, 1021, "float16"), (70000, 8, 64, "float32")])
+def test_rows_that_go_past_the_caches(N, k, D, dtype):
+    """Rows by place of more than 128 MiB, whole cache lines and not, in whole
+    numbers: sums of products below 2^24 leave fp32 nothing to round, so each
+    result is the exact one rounded once."""
+    import torch
+    import paper_2305_06942_amd as ebag
+    E = 40
+    assert N * k * D * (4 if dtype == "float32" else 2) > 128 << 20
+    g = torch.Generator(device="cuda").manual_seed(47)
+    t = getattr(torch, dtype)
+    whole = lambda *s: torch.randint(-9, 10, s, generator=g, device="cuda").to(t)  # noqa: E731
+    plan = ebag.MoePerm(N, k, E)
+    ids = torch.randint(-1, E, (N, k), generator=g, device="cuda", dtype=torch.int32)
+    offsets = torch.zeros(E + 1, dtype=torch.int32, device="cuda")
+    pos, src = torch.zeros_like(ids), torch.zeros(N * k, dtype=torch.int32, device="cuda")
+    plan.sort(ids, offsets, pos, src)
+    total = int(offsets[-1])
+    kept = (pos < total)[..., None]
+    assert 0 < total < N * k
+    x, w = whole(N, D), torch.randint(-9, 10, (N, k), generator=g, device="cuda").float()
+    xs, out = torch.full((N * k, D), float("nan"), dtype=t, device="cuda"), torch.full((N, D), float("nan"), dtype=t, device="cuda")
+    plan.dispatch(x, offsets, pos, xs)
+    want = torch.where(torch.arange(N * k, device="cuda")[:, None] < total, x[src.long() // k], 0)
+    assert torch.equal(xs, want)
+    ys = whole(N * k, D)
+    ys[total:] = float("nan")
+    rows = torch.where(kept, ys[pos.long()].float(), 0)
+    plan.combine(ys, offsets, pos, w, out)
+    assert torch.equal(out, (rows * w[..., None]).sum(1).to(t))
+    plan.dispatch_backward(ys, offsets, pos, out)
+    assert torch.equal(out, rows.sum(1).to(t))
+    dys, dw = torch.full_like(xs, float("nan")), torch.full_like(w, float("nan"))
+    plan.combine_backward(x, ys, offsets, pos, w, dys, dw)
+    assert torch.equal(dw, (rows * x.float()[:, None]).sum(2))
+    want = torch.zeros_like(dys)
+    want[pos.long().reshape(-1)] = torch.where(kept, w[..., None] * x.float()[:, None], 0).to(t).reshape(N * k, D)
+    assert torch.equal(dys, want)
+    plan.close()
