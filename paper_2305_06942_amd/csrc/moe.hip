@@ -8,6 +8,7 @@
 #include "common.h"
 #include "ebag_a2a.h"
 #include "in_flight.h"
+#include "lanes.h"
 #include "vec16.h"
 
 using namespace ebag;
@@ -443,10 +444,11 @@ __global__ __launch_bounds__(kRowThreads) void moe_combine_backward_kernel(const
     }
 #pragma unroll
     for (int i = 0; i < kAtOnce; ++i) {
-      for (int d = at.lanes / 2; d; d /= 2) dot[i] += __shfl_xor(dot[i], d);
+      if (j0 + i >= a.choices) continue;
+      dot[i] = sum_lanes(dot[i], at.lanes);
       if (spread) {
         if (at.lane == 0) dots[wave][i] = dot[i];
-      } else if (at.lane == 0 && j0 + i < a.choices) {
+      } else if (at.lane == 0) {
         a.dweights[at.token * a.choices + j0 + i] = dot[i];
       }
     }

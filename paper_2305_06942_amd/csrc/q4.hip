@@ -7,6 +7,7 @@
 
 #include "ebag_a2a.h"
 #include "gemv_ar.h"
+#include "lanes.h"
 #include "q4.h"
 
 using namespace ebag;
@@ -28,8 +29,6 @@ namespace {
 // repeat it; nothing they give is stored.
 //
 // The loads of a wave's next unit are under way while it works on one.
-
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 // Between lanes l, l + 16, l + 32, l + 48: w[t] of lane quarter c becomes w[c] of quarter t.
 __device__ __forceinline__ void transpose_words(vec16& w) {
@@ -499,18 +498,24 @@ int64_t most_tiles(int64_t rows, int64_t experts, int64_t cols) {
 }
 
 int launch_few(const gemv_ar_q4_plan* h, Q4Args a, hipStream_t stream) {
-  const int rt = h->glu ? 2 : 1, waves = 4, parts = h->dtype == EBAG_F32 ? 3 : 1;
+  const int rt = h->glu ? 2 : 1, parts = h->dtype == EBAG_F32 ? 3 : 1;
   const bool whole = h->group % 128 == 0;
   const int columns = whole ? 512 : 256;
   const int units = (a.K + columns - 1) / columns;
   const int rows = a.rows < 16 ? (int)a.rows : 16;
   const int64_t slots = a.offsets ? most_tiles(a.rows, h->experts, 16) : (a.rows + 15) / 16;
   const int64_t all_tiles = (a.out_rows + 15) / 16 * slots;
-  // A tile's waves: enough for 4096 in all, and for 1024 bytes of a row at a time.
+  // A tile's waves: 2048 in all, and with few rows 1024 bytes of a weight row at a time.  x is staged once for a
+  // workgroup's tiles, so with more rows of x fewer waves to a tile are better where there are tiles enough (20000 x 4096
+  // with 8 rows: four waves to a tile 20.8 us, two 16.8), and more where there are not (4096 x 4096 with 16 rows: four
+  // 10.7, eight 7.9; with one row 5.4 and 5.8).
+  const bool many = rows >= 4 || units >= 16;
+  const int waves = many && all_tiles * 4 < 2048 && units >= 8 ? 8 : 4;
+  // LDS: three workgroups on a CU, or one where there are no more of them than CUs.
+  auto fits = [&](int split) { return rows * parts * (2 * split * columns + 16) <= (waves == 8 ? 139264 : 49152); };
   a.split = 1;
-  while (a.split < waves && a.split * 2 <= units &&
-         (all_tiles * a.split < 4096 || a.row_bytes > 1024 * a.split) &&
-         rows * parts * (4 * a.split * columns + 16) <= 49152)
+  while (a.split < waves && a.split * 2 <= units && fits(a.split * 2) &&
+         (all_tiles * a.split < 2048 || (rows < 4 && a.row_bytes > 1024 * a.split)))
     a.split *= 2;
   // Its turns: about 2048 workgroups.
   const int64_t turn_rows = 16 * (waves / a.split);
@@ -549,10 +554,29 @@ int launch_tile(const gemv_ar_q4_plan* h, Q4Args a, int x_tiles, hipStream_t str
   return e == hipSuccess ? EBAG_OK : hipf(e, "launch the product with 4-bit weights");
 }
 
+// Which kernel: the one with the least time by what was measured at K = 4096 (all
+// grow with K alike): the kernel for few rows takes 8.0 ns for every 16 x 16 tile of
+// weight rows and rows of x; the matrix-product kernel with 32 rows of x 157 ns for
+// a workgroup, with 64 203 ns, and never less than 45 and 62 us, a workgroup's own
+// time.  Where a step of 128 columns has several scales: 12.5 ns, and with 64 rows 480
+// ns and 107 us.  (64 experts of 4096 x 2048, in us by the three: 12 rows each 94, 89, 101; 48
+// rows 280, 141, 129.  One matrix of 8192 x 4096: 64 rows 22, 48, 67; 256 rows 64, 49,
+// 67.)  An expert's rows fill their last tile half on average.
 int launch(const gemv_ar_q4_plan* h, const Q4Args& a, hipStream_t stream) {
-  const int64_t mean = a.rows / (a.offsets ? h->experts : 1);  // rows of a matrix
-  if (h->dtype == EBAG_F32 || mean < 32) return launch_few(h, a, stream);
-  return launch_tile(h, a, mean < 64 ? 1 : 2, stream);
+  if (h->dtype == EBAG_F32 || h->K >= 1 << 27) return launch_few(h, a, stream);
+  const bool whole = h->group % 128 == 0;
+  auto tiles = [&](double rows, double cols) {  // of `rows` weight rows and `cols` rows of x
+    const double experts = a.offsets ? h->experts : 1, some = a.rows < experts ? a.rows : experts;
+    const double slots = a.offsets ? a.rows / cols + experts / 2 : 0, all = (a.rows + (int)cols - 1) / (int)cols;
+    const double n = a.offsets ? (slots < some ? some : slots) : all;
+    return (double)((h->M + (int)rows - 1) / (int)rows) * (n < a.rows ? n : a.rows);
+  };
+  auto at_least = [](double v, double least) { return v < least ? least : v; };
+  const double few = tiles(16, 16) * (whole ? 0.0080 : 0.0125);
+  const double one = at_least(tiles(kQ4TileRows, 32) * 0.157, 45);
+  const double two = at_least(tiles(kQ4TileRows, 64) * (whole ? 0.203 : 0.48), whole ? 62 : 107);
+  if (few <= two && (few <= one || !whole)) return launch_few(h, a, stream);
+  return launch_tile(h, a, whole && one <= two ? 1 : 2, stream);
 }
 
 }  // namespace

@@ -2,13 +2,13 @@
 #include <hip/hip_runtime.h>
 
 #include "gemv_ar.h"
+#include "lanes.h"
 #include "q4.h"
 
 namespace ebag {
 namespace {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kStep = 128;   // columns of a step
@@ -39,21 +39,6 @@ __device__ __forceinline__ float sum8(const vec16& v) {
   return ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
 }
 
-template <int CTRL>
-__device__ __forceinline__ float add_lane(float v) {
-  return v + __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), CTRL, 0xf, 0xf, true));
-}
-
-// The sum over 4 or 16 neighbouring lanes, in each of them.
-template <int LANES>
-__device__ __forceinline__ float sum_lanes(float v) {
-  v = add_lane<0xB1>(v);   // quad_perm 1 0 3 2
-  v = add_lane<0x4E>(v);   // quad_perm 2 3 0 1
-  if (LANES == 4) return v;
-  v = add_lane<0x141>(v);  // row_half_mirror
-  return add_lane<0x140>(v);  // row_mirror
-}
-
 // A float as the first three elements of a vector, exactly: three bf16 (8 bits
 // each), or three fp16 (11 bits each).
 template <int DT>
@@ -69,7 +54,8 @@ __device__ __forceinline__ vec16 three_parts(float f) {
 }
 
 // WHOLE: a group is a multiple of 128 columns, so a step has one scale; otherwise
-// every block of 32 columns has its own.
+// every block of 32 columns has its own (only with 64 rows of x: with 32 the kernel
+// for few rows is never slower).
 template <int DT, int NT, bool WHOLE>
 struct Tile {
   static constexpr int BN = 32 * NT;                  // rows of x
@@ -184,7 +170,7 @@ __global__ __launch_bounds__(kThreads, 2) void q4_tile_kernel(const Q4Args a) {
     char* row = to + (tid >> 4) * C::PITCH;
 #pragma unroll
     for (int i = 0; i < C::STAGED; ++i) {
-      const float s = sum_lanes<WHOLE ? 16 : 4>(sum8<DT>(v[i]));
+      const float s = sum_lanes(sum8<DT>(v[i]), WHOLE ? 16 : 4);
       mine = i == pick ? s : mine;
       *reinterpret_cast<vec16*>(row + 16 * i * C::PITCH + chunk * 16) = pair_order(v[i]);
     }
@@ -295,18 +281,18 @@ __global__ __launch_bounds__(kThreads, 2) void q4_tile_kernel(const Q4Args a) {
 
 typedef void (*tile_fn)(const Q4Args);
 
-template <int DT, int NT>
-tile_fn pick(bool whole, bool zeros) {
-  return whole ? (zeros ? q4_tile_kernel<DT, NT, true, true> : q4_tile_kernel<DT, NT, true, false>)
-               : (zeros ? q4_tile_kernel<DT, NT, false, true> : q4_tile_kernel<DT, NT, false, false>);
+template <int DT>
+tile_fn pick(int x_tiles, bool whole, bool zeros) {
+  if (!whole) return zeros ? q4_tile_kernel<DT, 2, false, true> : q4_tile_kernel<DT, 2, false, false>;
+  if (x_tiles == 1) return zeros ? q4_tile_kernel<DT, 1, true, true> : q4_tile_kernel<DT, 1, true, false>;
+  return zeros ? q4_tile_kernel<DT, 2, true, true> : q4_tile_kernel<DT, 2, true, false>;
 }
 
 }  // namespace
 
 void launch_q4_tile(const Q4Args& a, int dtype, int x_tiles, unsigned grid, hipStream_t stream) {
   const bool whole = a.group % 128 == 0;
-  const tile_fn fn = dtype == EBAG_F16 ? (x_tiles == 1 ? pick<1, 1>(whole, a.zeros) : pick<1, 2>(whole, a.zeros))
-                                       : (x_tiles == 1 ? pick<2, 1>(whole, a.zeros) : pick<2, 2>(whole, a.zeros));
+  const tile_fn fn = dtype == EBAG_F16 ? pick<1>(x_tiles, whole, a.zeros) : pick<2>(x_tiles, whole, a.zeros);
   hipLaunchKernelGGL(fn, dim3(grid), dim3(kThreads), 0, stream, a);
 }
 

@@ -140,6 +140,24 @@ def test_long_rows_and_many_weight_rows():
     _forward(rng, 2, 20011, 160, 32, "float16", True, 0, True, y_dtype="float32")
 
 
+@pytest.mark.parametrize("dtype", TYPES[1:])
+@pytest.mark.parametrize("rows,M,K,group,zeros,glu", [
+    (400, 4100, 300, 128, True, 0), (389, 4610, 127, 128, False, 0), (400, 4100, 641, 256, False, 1),
+    (1000, 4100, 700, 256, True, 0), (1027, 4098, 256, 128, True, 1), (1000, 8200, 333, 32, True, 0), (1010, 8202, 224, 96, False, 1)])
+def test_forward_of_many_rows(rows, M, K, group, zeros, glu, dtype):
+    """Products large enough for the matrix-product kernel, in both its widths."""
+    _forward(np.random.default_rng([60, rows, M, K]), rows, M, K, group, dtype, zeros, glu, False,
+             step=5 if K % 2 else 0, shift=K % 2)
+
+
+@pytest.mark.parametrize("dtype", TYPES[1:])
+def test_forward_of_many_rows_exact(dtype):
+    rng = np.random.default_rng(61)
+    _forward(rng, 420, 4099, 260, 128, dtype, True, 0, True, y_dtype="float32", step=3, shift=1)
+    _forward(rng, 1001, 4099, 384, 128, dtype, False, 0, True, y_dtype="float32")
+    _forward(rng, 1001, 8199, 130, 64, dtype, True, 0, True, y_dtype="float32")
+
+
 def _offsets(rng, E, S, kept, empty):
     n = np.zeros(E, dtype=np.int64)
     live = rng.permutation(E)[:max(1, E - empty)]
@@ -180,6 +198,31 @@ def test_experts(E, N, k, M, K, group, zeros, glu, dropped, gather, dtype):
     assert bool((y[off[-1]:] == 0).all())
     _untouched(buf, S, wide, wide + 1, 3)
     plan.close()
+
+
+@pytest.mark.parametrize("dtype", TYPES[1:])
+@pytest.mark.parametrize("gather", [False, True])
+@pytest.mark.parametrize("E,N,k,M,K,group,zeros,glu,dropped", [
+    (40, 300, 2, 4098, 200, 128, True, 1, 40), (9, 700, 2, 4100, 260, 128, False, 0, 0), (9, 1400, 2, 4098, 161, 32, True, 1, 77),
+    (100, 600, 4, 1100, 384, 384, True, 0, 300)])
+def test_experts_of_many_rows(E, N, k, M, K, group, zeros, glu, dropped, gather, dtype):
+    test_experts(E, N, k, M, K, group, zeros, glu, dropped, gather, dtype)
+
+
+def test_small_fp16_values_count():
+    """fp16 x below its normal range (2^-14) is a sum like any other, in both kernels."""
+    import torch
+    import paper_2305_06942_amd as ebag
+    rng = np.random.default_rng(62)
+    for rows, M in ((3, 64), (1000, 4096)):
+        K = 256
+        plan = ebag.Q4Gemv(M, K, 128, _abi("float16"))
+        w = Weights(rng, 1, M, K, 128, "float16", True)
+        x = torch.from_numpy(rng.integers(-1000, 1001, size=(rows, K)) * 2.0 ** -24).half().cuda()
+        y = torch.empty((rows, M), device="cuda")
+        plan.forward(w.codes, w.scales, w.zeros, x, y)
+        _check(y, *_want(x.double().cpu().numpy(), w, 0, 0), "float32")
+        plan.close()
 
 
 def test_rows_are_independent_and_infinities_stay_their_own():
