@@ -517,10 +517,11 @@ int launch_few(const gemv_ar_q4_plan* h, Q4Args a, hipStream_t stream) {
   while (a.split < waves && a.split * 2 <= units && fits(a.split * 2) &&
          (all_tiles * a.split < 2048 || (rows < 4 && a.row_bytes > 1024 * a.split)))
     a.split *= 2;
-  // Its turns: about 2048 workgroups.
+  // Its turns: about 2048 workgroups, or 1024 of twice the weights (128 experts of 2 x 1024 x 2048, two rows each: 66
+  // us with 2048, 63.5 with 1024, 60 with 512; 64 experts of 4096 x 2048, four rows each: 59, 66 and 102 us).
   const int64_t turn_rows = 16 * (waves / a.split);
   const int64_t all_turns = (a.out_rows + turn_rows - 1) / turn_rows;
-  int64_t turns = all_turns * slots / 2048;
+  int64_t turns = all_turns * slots / (rt == 2 ? 1024 : 2048);
   turns = turns < 1 ? 1 : turns > all_turns ? all_turns : turns;
   a.turns = (int)turns;
   const int64_t tiles = (all_turns + turns - 1) / turns;
