@@ -135,34 +135,53 @@ __device__ __forceinline__ void split_f32(const vec16& lo, const vec16& hi, vec1
     for (int j = 0; j < 4; ++j) parts[p][j] = __builtin_amdgcn_perm(cut[p][j + 4], cut[p][j], 0x07060302u);
 }
 
+// A vector without its first `bytes` (0 to 15), zeros behind.
+__device__ __forceinline__ vec16 without_first(const vec16& v, int bytes) {
+  uint64_t lo = v[0] | (uint64_t)v[1] << 32, hi = v[2] | (uint64_t)v[3] << 32;
+  if (bytes >= 8) {
+    lo = hi;
+    hi = 0;
+  }
+  const int s = 8 * (bytes & 7);
+  if (s) lo = lo >> s | hi << (64 - s);
+  hi >>= s;
+  return vec16{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+}
+
 // 16 bytes of codes; what lies behind a row's end is not used, what lies
 // behind the last matrix is not read.
 __device__ __forceinline__ vec16 load_codes_end(const Q4Args& a, const uint8_t* p) {
-  if (p + 16 <= a.codes + a.codes_bytes) return load16(reinterpret_cast<const char*>(p));
+  const int64_t left = a.codes + a.codes_bytes - p;
+  if (left >= 16) return load16(reinterpret_cast<const char*>(p));
+  if (left <= 0) return vec16{0, 0, 0, 0};
+  if (a.codes_bytes >= 16) return without_first(load16(reinterpret_cast<const char*>(p + left - 16)), 16 - (int)left);
   vec16 r = {0, 0, 0, 0};
-  for (int i = 0; i < 16; ++i)
-    if (p + i < a.codes + a.codes_bytes) r[i / 4] |= (uint32_t)p[i] << (8 * (i % 4));
+  for (int i = 0; i < left; ++i) r[i / 4] |= (uint32_t)p[i] << (8 * (i % 4));
   return r;
 }
 
-// The first n of eight elements of x, zeros behind them.
+// The first n (at most 8) of eight elements of a row of x of K, zeros behind them.
 template <int DT>
-__device__ __forceinline__ void load_x(const char* p, int n, vec16* v) {
-  constexpr int VECS = DT == 0 ? 2 : 1;
-  if (n >= 8) {
+__device__ __forceinline__ void load_x(const char* p, int n, int K, vec16* v) {
+  constexpr int VECS = DT == 0 ? 2 : 1, N = DT == 0 ? 4 : 8, ELT = 16 / N;
 #pragma unroll
-    for (int i = 0; i < VECS; ++i) v[i] = load16(p + 16 * i);
-    return;
-  }
+  for (int i = 0; i < VECS; ++i) {
+    const int have = n - i * N;
+    const char* at = p + 16 * i;
+    v[i] = vec16{0, 0, 0, 0};
+    if (have >= N)
+      v[i] = load16(at);
+    else if (have > 0 && K >= N)  // the row's last vector, without what is before `at`
+      v[i] = without_first(load16(at + have * ELT - 16), 16 - have * ELT);
+    else if (have > 0)
 #pragma unroll
-  for (int i = 0; i < VECS; ++i) v[i] = vec16{0, 0, 0, 0};
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    if (i >= n) continue;
-    if (DT == 0)
-      v[i / 4][i % 4] = reinterpret_cast<const uint32_t*>(p)[i];
-    else
-      v[0][i / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[i] << (16 * (i % 2));
+      for (int e = 0; e < N; ++e) {
+        if (e >= have) continue;
+        if (DT == 0)
+          v[i][e % 4] = reinterpret_cast<const uint32_t*>(at)[e];
+        else
+          v[i][e / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(at)[e] << (16 * (e % 2));
+      }
   }
 }
 

@@ -51,7 +51,7 @@ __device__ __forceinline__ void gather_words(uint32_t w, uint32_t* all) {
   all[0] = lo[0]; all[1] = lo[1]; all[2] = hi[0]; all[3] = hi[1];
 }
 
-constexpr int kFewThreads = 512;
+constexpr int kFewThreads = 512, kCuLds = 160 * 1024;
 
 // What a launch is compiled for.  WHOLE: a group is a multiple of 128 columns, so
 // a step of 128 has one scale.  ZEROS: there are zero points.
@@ -183,7 +183,7 @@ __device__ __forceinline__ void stage_x(const Q4Args& a, uint32_t first, int row
       int64_t row = a.src ? (int64_t)divide_by(a.by_choices, (uint32_t)a.src[first + r] & 0x7fffffffu) : (int64_t)(first + r);
       row = row < a.x_rows ? row : a.x_rows - 1;
       const int k = k0 + 8 * (int)c;
-      load_x<DT>(a.x + row * a.ldx + (int64_t)k * ELT, a.K - k, v[j]);
+      load_x<DT>(a.x + row * a.ldx + (int64_t)k * ELT, a.K - k, a.K, v[j]);
       to[j] = lds + r * pitch + c * 16;
     }
 #pragma unroll
@@ -511,8 +511,10 @@ int launch_few(const gemv_ar_q4_plan* h, Q4Args a, hipStream_t stream) {
   // 10.7, eight 7.9; with one row 5.4 and 5.8).
   const bool many = rows >= 4 || units >= 16;
   const int waves = many && all_tiles * 4 < 2048 && units >= 8 ? 8 : 4;
-  // LDS: three workgroups on a CU, or one where there are no more of them than CUs.
-  auto fits = [&](int split) { return rows * parts * (2 * split * columns + 16) <= (waves == 8 ? 139264 : 49152); };
+  // LDS: x and the waves' sums, two of each tile's; three workgroups on a CU, or one where there are no more of them
+  // than CUs.
+  const int sums = 2 * waves * rt * 64 * (int)sizeof(f32x4), most = waves == 8 ? kCuLds - sums : 49152;
+  auto fits = [&](int split) { return rows * parts * (2 * split * columns + 16) + 16 <= most; };
   a.split = 1;
   while (a.split < waves && a.split * 2 <= units && fits(a.split * 2) &&
          (all_tiles * a.split < 2048 || (rows < 4 && a.row_bytes > 1024 * a.split)))
@@ -537,7 +539,7 @@ int launch_few(const gemv_ar_q4_plan* h, Q4Args a, hipStream_t stream) {
   a.by_all = make_divisor(a.all_columns / 8);
   a.by_some = make_divisor(a.some_columns / 8);
   a.x_bytes = (int)(a.fit_rows < rows ? (room + 15) / 16 * 16 : rows * parts * (2 * (int64_t)a.all_columns + 16));
-  const size_t lds = a.x_bytes + (a.split > 1 ? 2 * waves * rt * 64 * sizeof(f32x4) : 0);
+  const size_t lds = a.x_bytes + (a.split > 1 ? sums : 0);
   const q4_fn fn = rt == 1 ? pick_few<1>(h->dtype, whole, a.zeros) : pick_few<2>(h->dtype, whole, a.zeros);
   hipLaunchKernelGGL(fn, dim3((unsigned)(tiles * slots)), dim3(64 * waves), lds, stream, a);
   const hipError_t e = hipGetLastError();

@@ -161,7 +161,7 @@ __global__ __launch_bounds__(kThreads, 2) void q4_tile_kernel(const Q4Args a) {
     }
     const int n = a.K - step * kStep - 8 * chunk;  // elements left
 #pragma unroll
-    for (int i = 0; i < C::STAGED; ++i) load_x<DT>(x[i] + (int64_t)step * (kStep * 2), n, &v[i]);
+    for (int i = 0; i < C::STAGED; ++i) load_x<DT>(x[i] + (int64_t)step * (kStep * 2), n, a.K, &v[i]);
   };
   auto store_rows = [&](const vec16* v, char* to) {
     // Lane `chunk` of a row (or of a quarter of it) finishes the sums of row number `chunk` % STAGED.

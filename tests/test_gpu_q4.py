@@ -134,6 +134,15 @@ def test_forward(rows, M, K, group, zeros, glu, dtype):
              step=5 if K % 2 else 0, shift=K % 2)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("glu", [0, 1])
+@pytest.mark.parametrize("group", [64, 128])
+@pytest.mark.parametrize("rows,M,K", [(16, 128, 4096), (12, 34, 8200), (5, 512, 12288), (16, 2048, 5000)])
+def test_forward_where_a_tile_has_eight_waves(rows, M, K, group, glu, dtype):
+    """Few weight rows: the launches that ask for the most LDS."""
+    _forward(np.random.default_rng([63, rows, M]), rows, M, K, group, dtype, True, glu, False)
+
+
 def test_long_rows_and_many_weight_rows():
     rng = np.random.default_rng(53)
     _forward(rng, 1, 48, 70001, 128, "bfloat16", True, 0, False)
