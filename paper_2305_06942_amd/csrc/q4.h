@@ -160,6 +160,16 @@ __device__ __forceinline__ vec16 load_codes_end(const Q4Args& a, const uint8_t* 
   return r;
 }
 
+// The same at a multiple of 4 bytes, in whole words: one is read if a byte of it is
+// in range, and zero otherwise.
+__device__ __forceinline__ vec16 load_words_end(const Q4Args& a, const uint8_t* p) {
+  vec16 r = {0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (p + 4 * i < a.codes + a.codes_bytes) r[i] = reinterpret_cast<const uint32_t*>(p)[i];
+  return r;
+}
+
 // The first n (at most 8) of eight elements of a row of x of K, zeros behind them.
 template <int DT>
 __device__ __forceinline__ void load_x(const char* p, int n, int K, vec16* v) {
@@ -240,6 +250,19 @@ __device__ __forceinline__ void store_y(const Q4Args& a, uint32_t n, int64_t m, 
 }
 
 __device__ __forceinline__ float silu(float v) { return v / (1.f + __expf(-v)); }
+
+typedef void (*q4_fn)(const Q4Args);
+
+// Which instance of the kernel for few rows a launch takes.
+struct Q4FewKind {
+  int tiles;    // of 16 weight rows of a wave: 1, or 2 with glu
+  bool whole;   // a group is a multiple of 128 columns
+  bool zeros;   // there are zero points
+  bool words;   // rows of codes begin at multiples of 4 bytes
+};
+q4_fn pick_q4_few_f32(const Q4FewKind& k);
+q4_fn pick_q4_few_f16(const Q4FewKind& k);
+q4_fn pick_q4_few_bf16(const Q4FewKind& k);
 
 // The matrix-product kernel for many rows of fp16 or bf16 x: a workgroup for
 // kQ4TileRows rows of weights (half as many outputs with glu) and 32 x_tiles (1 or

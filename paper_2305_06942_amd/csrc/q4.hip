@@ -1,5 +1,5 @@
 // Products with 4-bit weights (gemv_ar_q4_* of include/gemv_ar.h): rounding to 4
-// bits, and the kernel for few rows of x.
+// bits, and the host side: checks, launch shapes, the choice of kernel.
 #include <hip/hip_runtime.h>
 
 #include <climits>
@@ -7,365 +7,11 @@
 
 #include "ebag_a2a.h"
 #include "gemv_ar.h"
-#include "lanes.h"
 #include "q4.h"
 
 using namespace ebag;
 
 namespace {
-
-// ------------------------------------------------------------------- few rows
-//
-// A workgroup has RT tiles of 16 rows of weights and 16 rows of x; its
-// waves split K in units of 256 columns (a cache line of codes), wave w
-// taking units w, w + waves, ..., and join their sums in LDS at the end.  A
-// lane loads 16 bytes, 32 consecutive codes of row lane % 16; a transposition
-// between the four lanes of a row (lane / 16) then gives word t of each the
-// columns 32 t + 8 (lane / 16) .. + 8, the layout of a 16x16x32 matrix
-// instruction over 32 consecutive columns, which belong to one group.  x is
-// the first operand, so a lane holds sums of ONE weight row for four rows of x
-// and needs one scale per group: the four lanes of a row load those of four
-// blocks of 32 columns and pass them round.  Rows of a tile beyond the last one
-// repeat it; nothing they give is stored.
-//
-// The loads of a wave's next unit are under way while it works on one.
-
-// Between lanes l, l + 16, l + 32, l + 48: w[t] of lane quarter c becomes w[c] of quarter t.
-__device__ __forceinline__ void transpose_words(vec16& w) {
-  u32x2 s;
-  s = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
-  w[0] = s[0]; w[2] = s[1];
-  s = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
-  w[1] = s[0]; w[3] = s[1];
-  s = __builtin_amdgcn_permlane16_swap(w[0], w[1], false, false);
-  w[0] = s[0]; w[1] = s[1];
-  s = __builtin_amdgcn_permlane16_swap(w[2], w[3], false, false);
-  w[2] = s[0]; w[3] = s[1];
-}
-
-// The words of the four quarters, in each of them.
-__device__ __forceinline__ void gather_words(uint32_t w, uint32_t* all) {
-  const u32x2 half = __builtin_amdgcn_permlane32_swap(w, w, false, false);
-  const u32x2 lo = __builtin_amdgcn_permlane16_swap(half[0], half[0], false, false);
-  const u32x2 hi = __builtin_amdgcn_permlane16_swap(half[1], half[1], false, false);
-  all[0] = lo[0]; all[1] = lo[1]; all[2] = hi[0]; all[3] = hi[1];
-}
-
-constexpr int kFewThreads = 512, kCuLds = 160 * 1024;
-
-// What a launch is compiled for.  WHOLE: a group is a multiple of 128 columns, so
-// a step of 128 has one scale.  ZEROS: there are zero points.
-template <int DT_, int RT_, bool WHOLE_, bool ZEROS_>
-struct FewShape {
-  static constexpr int DT = DT_, RT = RT_;
-  static constexpr bool WHOLE = WHOLE_, ZEROS = ZEROS_;
-  static constexpr int STEPS = WHOLE ? 4 : 2;     // of a unit
-  static constexpr int SCALES = WHOLE ? 1 : STEPS;  // loads of scales of a unit: four lanes of a row load one each
-  static constexpr int COLUMNS = 128 * STEPS;
-};
-
-// Where a lane of a wave with RT tiles of weight rows loads its next unit from.
-template <class C>
-struct Few {
-  const uint8_t* codes[C::RT];  // its row of weights, its quarter's bytes
-  const char* scales[C::RT];    // that row's first scale
-  const uint8_t* zeros[C::RT];  // and zero
-  int unit, split;
-
-  __device__ __forceinline__ void advance() {
-#pragma unroll
-    for (int rt = 0; rt < C::RT; ++rt) codes[rt] += split * (C::COLUMNS / 2);
-    unit += split;
-  }
-};
-
-// A unit's weights, as loaded.  WHOLE: a lane has the scale and zero of step
-// `quarter`; otherwise those of block `quarter` of each step.
-template <class C>
-struct Unit {
-  vec16 w[C::STEPS][C::RT];
-  uint32_t scale[C::SCALES][C::RT], zero[C::SCALES][C::RT];
-};
-
-// END: the unit passes the end of K.
-template <bool END, class C>
-__device__ __forceinline__ void load_weights(const Q4Args& a, const Few<C>& f, Unit<C>& o) {
-  const int quarter = (threadIdx.x & 63) >> 4;
-#pragma unroll
-  for (int s = 0; s < C::STEPS; ++s)
-#pragma unroll
-    for (int rt = 0; rt < C::RT; ++rt) {
-      const uint8_t* p = f.codes[rt] + s * 64;
-      o.w[s][rt] = END ? load_codes_end(a, p) : load16(reinterpret_cast<const char*>(p));
-    }
-#pragma unroll
-  for (int s = 0; s < C::SCALES; ++s) {
-    const int block = f.unit * (4 * C::STEPS) + (C::WHOLE ? 4 * quarter : 4 * s + quarter);
-    uint32_t g = divide_by(a.by_group_blocks, (uint32_t)block);
-    if (END) g = g < (uint32_t)a.groups ? g : a.groups - 1;
-#pragma unroll
-    for (int rt = 0; rt < C::RT; ++rt) {
-      o.scale[s][rt] = C::DT == 0 ? reinterpret_cast<const uint32_t*>(f.scales[rt])[g]
-                                  : (uint32_t)reinterpret_cast<const uint16_t*>(f.scales[rt])[g];
-      o.zero[s][rt] = C::ZEROS ? f.zeros[rt][g] : 8u;
-    }
-  }
-}
-
-// The unit's products, added to the sums.  x: the lane's row of x in LDS, the
-// unit's columns; the parts of fp32 x are `pitch` bytes apart.
-template <class C>
-__device__ __forceinline__ void multiply(const CodeBits<C::DT>& bits, Unit<C>& o, const char* x, int pitch, f32x4* sum) {
-  typedef Q4Type<C::DT> Q;
-  typedef Type<C::DT> T;
-  constexpr int PARTS = Q::PARTS, RT = C::RT;
-  constexpr bool F32 = C::DT == 0;
-  const vec16 ones = {Q::ONES, Q::ONES, Q::ONES, Q::ONES};
-  uint32_t all[RT][4], zero[RT][4];  // scale, and the zero above it or in a word of its own
-#pragma unroll
-  for (int s = 0; s < C::STEPS; ++s) {
-    float scale[RT][4], off[RT][4];
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      transpose_words(o.w[s][rt]);
-      if (!C::WHOLE || s == 0) {
-        gather_words(o.scale[s][rt] | (C::ZEROS && !F32 ? o.zero[s][rt] << 16 : 0u), all[rt]);
-        if (C::ZEROS && F32) gather_words(o.zero[s][rt], zero[rt]);
-      }
-#pragma unroll
-      for (int t = 0; t < (C::WHOLE ? 1 : 4); ++t) {
-        const int at = C::WHOLE ? s : t;
-        scale[rt][t] = F32 ? __uint_as_float(all[rt][at])
-                           : T::widen(__builtin_bit_cast(typename T::elt, (typename Bits<C::DT>::type)all[rt][at]));
-        off[rt][t] = C::ZEROS ? -Q::BASE - (float)(F32 ? zero[rt][at] : all[rt][at] >> 16) : -Q::BASE - 8.f;
-      }
-    }
-    f32x4 v[RT], xsum;
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      vec16 xs[PARTS];
-#pragma unroll
-      for (int p = 0; p < PARTS; ++p) xs[p] = *reinterpret_cast<const vec16*>(x + p * pitch + (s * 4 + t) * 64);
-      if (!C::WHOLE || t == 0) xsum = f32x4{0, 0, 0, 0};
-#pragma unroll
-      for (int p = 0; p < PARTS; ++p) xsum = Q::mfma(xs[p], ones, xsum);
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        const vec16 q = unpack_codes(bits, o.w[s][rt][t]);
-        if (!C::WHOLE || t == 0) v[rt] = f32x4{0, 0, 0, 0};
-#pragma unroll
-        for (int p = 0; p < PARTS; ++p) v[rt] = Q::mfma(xs[p], q, v[rt]);
-        if (C::WHOLE && t < 3) continue;
-        const int g = C::WHOLE ? 0 : t;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          sum[rt][i] = __builtin_fmaf(scale[rt][g], __builtin_fmaf(off[rt][g], xsum[i], v[rt][i]), sum[rt][i]);
-      }
-    }
-  }
-}
-
-// Rows first .. first + rows of x into LDS, columns k0 .. k0 + cols (by8: cols / 8),
-// in pair order, zeros behind column K; row r at r * pitch, further parts of
-// fp32 rows * pitch behind.
-template <int DT>
-__device__ __forceinline__ void stage_x(const Q4Args& a, uint32_t first, int rows, int k0, const Divisor& by8, int pitch,
-                                        char* lds) {
-  constexpr int ELT = DT == 0 ? 4 : 2, VECS = DT == 0 ? 2 : 1, PARTS = Q4Type<DT>::PARTS, AT_ONCE = 4;
-  const uint32_t n = rows * by8.d;
-  for (uint32_t i0 = threadIdx.x; i0 < n; i0 += AT_ONCE * blockDim.x) {
-    vec16 v[AT_ONCE][VECS];
-    char* to[AT_ONCE];
-#pragma unroll
-    for (int j = 0; j < AT_ONCE; ++j) {
-      const uint32_t i = i0 + j * blockDim.x < n ? i0 + j * blockDim.x : n - 1;
-      const uint32_t r = divide_by(by8, i), c = i - r * by8.d;
-      int64_t row = a.src ? (int64_t)divide_by(a.by_choices, (uint32_t)a.src[first + r] & 0x7fffffffu) : (int64_t)(first + r);
-      row = row < a.x_rows ? row : a.x_rows - 1;
-      const int k = k0 + 8 * (int)c;
-      load_x<DT>(a.x + row * a.ldx + (int64_t)k * ELT, a.K - k, a.K, v[j]);
-      to[j] = lds + r * pitch + c * 16;
-    }
-#pragma unroll
-    for (int j = 0; j < AT_ONCE; ++j) {
-      vec16 parts[PARTS];
-      if (DT == 0)
-        split_f32(v[j][0], v[j][VECS - 1], parts);
-      else
-        parts[0] = pair_order(v[j][0]);
-#pragma unroll
-      for (int p = 0; p < PARTS; ++p) *reinterpret_cast<vec16*>(to[j] + p * rows * pitch) = parts[p];
-    }
-  }
-}
-
-template <class C>
-__global__ __launch_bounds__(kFewThreads, C::RT == 1 ? 4 : 2) void q4_few_kernel(const Q4Args a) {
-  constexpr int DT = C::DT, RT = C::RT;
-  extern __shared__ __attribute__((aligned(16))) char lds[];  // x; the waves' sums [2][waves][RT][64]
-  const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int r16 = lane & 15, quarter = lane >> 4;
-  const int tiles = waves / a.split, own = wave / a.split, part = wave - own * a.split;
-  const uint32_t slot = divide_by(a.by_tiles, blockIdx.x);
-  int expert;
-  uint32_t first, end;
-  if (!find_tile(a, slot, 16, &expert, &first, &end)) return;
-  // The wave's rows of weights m0 + 16 rt + r16 of the outputs; with glu, its tiles alternate between gate and up rows.
-  const int pair = a.glu ? 2 : 1, tile_rows = 16 * RT / pair, turn_rows = tiles * tile_rows;
-  const int64_t wg_m0 = (int64_t)(blockIdx.x - slot * a.by_tiles.d) * ((int64_t)a.turns * turn_rows);
-  if (expert == a.experts) {
-    const uint32_t cols = a.turns * turn_rows;
-    for (uint32_t i = threadIdx.x; i < 16 * cols; i += blockDim.x) {
-      const uint32_t n = first + i / cols;
-      const int64_t m = wg_m0 + i % cols;
-      if (n < end && m < a.out_rows) store_y<DT>(a, n, m, 0.f);
-    }
-    return;
-  }
-  int turns = a.turns;  // of this workgroup: up to its last rows of weights
-  while (turns > 1 && wg_m0 + (int64_t)(turns - 1) * turn_rows >= a.out_rows) --turns;
-  int64_t m0 = wg_m0 + own * tile_rows;
-  Few<C> f;
-  f.split = a.split;
-  auto start = [&](int64_t from) {  // the first unit of the tile at weight row `from`
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      int64_t m = from + 16 * (rt / pair) + r16;
-      m = m < a.out_rows ? m : a.out_rows - 1;
-      if (pair == 2 && (rt & 1)) m += a.out_rows;
-      m += (int64_t)expert * a.M;
-      f.codes[rt] = a.codes + m * a.row_bytes + part * (C::COLUMNS / 2) + quarter * 16;
-      f.scales[rt] = a.scales + m * a.groups * (DT == 0 ? 4 : 2);
-      f.zeros[rt] = a.zeros ? a.zeros + m * a.groups : a.codes;
-    }
-    f.unit = part;
-  };
-  const int rows = end - first < 16 ? end - first : 16;
-  // All columns of x at once where they fit, or a unit or more for each of a tile's waves at a time.
-  const bool fits = rows <= a.fit_rows;
-  const int columns = fits ? a.all_columns : a.some_columns, pitch = 2 * columns + 16;
-  const int whole = a.K / C::COLUMNS;
-  const char* x = lds + (r16 < rows ? r16 : rows - 1) * pitch + quarter * 16;
-  f32x4* sums = reinterpret_cast<f32x4*>(lds + a.x_bytes);
-  const CodeBits<DT> bits;
-  f32x4 sum[RT];
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt) sum[rt] = f32x4{0, 0, 0, 0};
-  Unit<C> even, odd;
-  int turn = 0;
-
-  auto times = [&](Unit<C>& o, int unit) { multiply(bits, o, x + unit * (2 * C::COLUMNS), rows * pitch, sum); };
-  // A tile's end: its waves join their sums, and it is stored.  Lane (r16, quarter) has rows 4 quarter .. + 4 of x.
-  auto finish = [&]() {
-    if (a.split > 1) {
-      f32x4* now = sums + (turn & 1) * (waves * RT * 64);  // the other half may still be read from
-      if (part) {
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) now[(wave * RT + rt) * 64 + lane] = sum[rt];
-      }
-      __syncthreads();
-      if (!part) {
-        for (int w = wave + 1; w < wave + a.split; ++w)
-#pragma unroll
-          for (int rt = 0; rt < RT; ++rt) sum[rt] += now[(w * RT + rt) * 64 + lane];
-      }
-    }
-    if (!part) {
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        if (pair == 2 && (rt & 1)) continue;
-        const int64_t m = m0 + 16 * (rt / pair) + r16;
-        if (m >= a.out_rows) continue;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const uint32_t n = first + 4 * quarter + k;
-          if (n < end) store_y<DT>(a, n, m, pair == 2 ? silu(sum[rt][k]) * sum[rt + 1 < RT ? rt + 1 : rt][k] : sum[rt][k]);
-        }
-      }
-    }
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) sum[rt] = f32x4{0, 0, 0, 0};
-    ++turn;
-    m0 += turn_rows;
-  };
-
-  if (fits && whole * C::COLUMNS == a.K && part < whole) {
-    // Whole units, two in turn through all turns: each is loaded while the other one is worked on.
-    start(m0);
-    load_weights<false>(a, f, even);
-    stage_x<DT>(a, first, rows, 0, a.by_all, pitch, lds);
-    __syncthreads();
-    bool more, ends;
-    int now;
-    auto next = [&]() {
-      now = f.unit;
-      f.advance();
-      ends = f.unit >= whole;
-      more = !ends || turn + 1 < turns;
-      if (ends && more) start(m0 + turn_rows);
-    };
-    for (;;) {
-      next();
-      if (!more) {
-        times(even, now);
-        break;
-      }
-      load_weights<false>(a, f, odd);
-      times(even, now);
-      if (ends) finish();
-      next();
-      if (!more) {
-        times(odd, now);
-        break;
-      }
-      load_weights<false>(a, f, even);
-      times(odd, now);
-      if (ends) finish();
-    }
-    finish();
-    return;
-  }
-  // K that ends inside a unit, or more of x than fits.
-  for (int t = 0; t < turns; ++t) {
-    start(m0);
-    for (int k0 = 0; k0 < a.K; k0 += columns) {
-      const int first_unit = k0 / C::COLUMNS, end_unit = first_unit + columns / C::COLUMNS;
-      const int last = end_unit < whole ? end_unit : whole;
-      if (f.unit < last) load_weights<false>(a, f, even);
-      if (t == 0 || !fits) {
-        if (t || k0) __syncthreads();
-        stage_x<DT>(a, first, rows, k0, fits ? a.by_all : a.by_some, pitch, lds);
-        __syncthreads();
-      }
-      if (f.unit < last) {
-        for (;;) {
-          int now = f.unit;
-          f.advance();
-          if (f.unit >= last) {
-            times(even, now - first_unit);
-            break;
-          }
-          load_weights<false>(a, f, odd);
-          times(even, now - first_unit);
-          now = f.unit;
-          f.advance();
-          if (f.unit >= last) {
-            times(odd, now - first_unit);
-            break;
-          }
-          load_weights<false>(a, f, even);
-          times(odd, now - first_unit);
-        }
-      }
-      if (f.unit == whole && whole * C::COLUMNS < a.K && whole < end_unit) {
-        load_weights<true>(a, f, even);
-        times(even, whole - first_unit);
-      }
-    }
-    finish();
-  }
-}
 
 // ------------------------------------------------------------------- to 4 bits
 
@@ -418,18 +64,7 @@ __global__ __launch_bounds__(256) void q4_quantize_kernel(const QuantArgs a) {
   }
 }
 
-typedef void (*q4_fn)(const Q4Args);
-
-template <int DT, int RT>
-q4_fn pick_shape(bool whole, bool zeros) {
-  return whole ? (zeros ? q4_few_kernel<FewShape<DT, RT, true, true>> : q4_few_kernel<FewShape<DT, RT, true, false>>)
-               : (zeros ? q4_few_kernel<FewShape<DT, RT, false, true>> : q4_few_kernel<FewShape<DT, RT, false, false>>);
-}
-
-template <int RT>
-q4_fn pick_few(int dt, bool whole, bool zeros) {
-  return dt == EBAG_F32 ? pick_shape<0, RT>(whole, zeros) : dt == EBAG_F16 ? pick_shape<1, RT>(whole, zeros) : pick_shape<2, RT>(whole, zeros);
-}
+constexpr int kCuLds = 160 * 1024;
 
 int hipf(hipError_t e, const char* what) { return fail(EBAG_EHIP, "%s: %s", what, hipGetErrorString(e)); }
 
@@ -540,7 +175,8 @@ int launch_few(const gemv_ar_q4_plan* h, Q4Args a, hipStream_t stream) {
   a.by_some = make_divisor(a.some_columns / 8);
   a.x_bytes = (int)(a.fit_rows < rows ? (room + 15) / 16 * 16 : rows * parts * (2 * (int64_t)a.all_columns + 16));
   const size_t lds = a.x_bytes + (a.split > 1 ? sums : 0);
-  const q4_fn fn = rt == 1 ? pick_few<1>(h->dtype, whole, a.zeros) : pick_few<2>(h->dtype, whole, a.zeros);
+  const Q4FewKind kind = {rt, whole, a.zeros != nullptr, a.row_bytes % 4 == 0 && reinterpret_cast<uintptr_t>(a.codes) % 4 == 0};
+  const q4_fn fn = h->dtype == EBAG_F32 ? pick_q4_few_f32(kind) : h->dtype == EBAG_F16 ? pick_q4_few_f16(kind) : pick_q4_few_bf16(kind);
   hipLaunchKernelGGL(fn, dim3((unsigned)(tiles * slots)), dim3(64 * waves), lds, stream, a);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? EBAG_OK : hipf(e, "launch the product with 4-bit weights");

@@ -3,14 +3,18 @@
 Exact inputs: whole x below 2^7, scales that are powers of two and sums below
 2^24 leave fp32 nothing to round, so such results are compared bit for bit.
 
-Others: a code goes through the sums as 16 + q (at most 31) and the zero's
-part comes off again, so fp32 sums terms of up to 62 s |x| in all.  The longest
-chain has 128 products of a group, a multiply-add pair per 32 columns and at
-most 16 partial sums; with 2^-23 for each (sums of a matrix instruction need
-not be rounded to nearest), |sum - want| <= b = (128 + K / 16 + 16) 2^-23 * 62
-sum_k s |x|.  silu(g) = g / (1 + exp(-g)) with an exponential good to (|g| + 8)
-2^-22 and a slope of at most 1.1 carries b on.  Rounding to the storage type keeps
-order, so a result lies between want - b and want + b, both rounded."""
+Others: with fp32 x a code goes through the sums as 16 + q (at most 31) and the
+zero's part comes off again, so fp32 sums terms of up to 62 s |x| in all.  The
+longest chain has 128 products of a group, a multiply-add pair per 32 columns
+and at most 16 partial sums; with 2^-23 for each (sums of a matrix instruction
+need not be rounded to nearest), |sum - want| <= b = (128 + K / 16 + 16) 2^-23 *
+62 sum_k s |x|.  With fp16 and bf16 x a code goes as 64 + q or 128 + q, terms of
+up to 286 s |x|, but a matrix instruction adds 32 columns: 512 columns are 16
+steps, and 16 * 286 < 128 * 62, so b holds there too.
+
+silu(g) = g / (1 + exp(-g)) with an exponential good to (|g| + 8) 2^-22 and a
+slope of at most 1.1 carries b on.  Rounding to the storage type keeps order, so
+a result lies between want - b and want + b, both rounded."""
 import numpy as np
 import pytest
 
@@ -33,9 +37,9 @@ def _abi(dtype):
 
 
 class Weights:
-    """4-bit weights on the GPU, at an odd address, and their values in 64 bits."""
+    """4-bit weights on the GPU, `at` bytes behind an allocation's start, and their values in 64 bits."""
 
-    def __init__(self, rng, E, M, K, group, dtype, zeros, exact=False):
+    def __init__(self, rng, E, M, K, group, dtype, zeros, exact=False, at=3):
         import torch
         rb, groups = (K + 1) // 2, -(-K // group)
         codes = rng.integers(0, 256, size=(E, M, rb), dtype=np.uint8)
@@ -44,8 +48,8 @@ class Weights:
         else:
             scales = rng.uniform(0.5, 1.5, size=(E, M, groups)) / (4.6 * np.sqrt(K))
         z = rng.integers(0, 16, size=(E, M, groups), dtype=np.uint8) if zeros else None
-        buf = torch.zeros(codes.size + 3, dtype=torch.uint8, device="cuda")
-        self.codes = buf[3:].view(E, M, rb)
+        buf = torch.zeros(codes.size + at, dtype=torch.uint8, device="cuda")
+        self.codes = buf[at:].view(E, M, rb)
         self.codes.copy_(torch.from_numpy(codes))
         self.scales = torch.from_numpy(scales).to(getattr(torch, dtype)).cuda()
         self.zeros = None if z is None else torch.from_numpy(z).cuda()
@@ -105,11 +109,13 @@ def _forward(rng, rows, M, K, group, dtype, zeros, glu, exact, y_dtype=None, ste
     w = Weights(rng, 1, M, K, group, dtype, zeros, exact)
     x = _x(rng, rows, K, dtype, exact, K + step, shift)
     wide = M // 2 if glu else M
-    y, buf = _strided(rows, wide, y_dtype, wide + step, shift)
-    plan.forward(w.codes, w.scales, w.zeros, x, y)
     want, b = _want(x.double().cpu().numpy(), w, 0, glu)
-    _check(y, want, 0 * b if exact else b, y_dtype)
-    _untouched(buf, rows, wide, wide + step, shift)
+    aligned = w.codes.clone()  # and on a boundary, where rows of a multiple of 4 bytes are too
+    for codes in (w.codes, aligned):
+        y, buf = _strided(rows, wide, y_dtype, wide + step, shift)
+        plan.forward(codes, w.scales, w.zeros, x, y)
+        _check(y, want, 0 * b if exact else b, y_dtype)
+        _untouched(buf, rows, wide, wide + step, shift)
     plan.close()
 
 
@@ -191,7 +197,7 @@ def test_experts(E, N, k, M, K, group, zeros, glu, dropped, gather, dtype):
     off = _offsets(rng, E, S, S - dropped, E // 4)
     src = rng.permutation(S).astype(np.int32)
     plan = ebag.Q4Gemv(M, K, group, _abi(dtype), experts=E, glu=glu)
-    w = Weights(rng, E, M, K, group, dtype, zeros)
+    w = Weights(rng, E, M, K, group, dtype, zeros, at=int(rng.integers(0, 4)) if gather else 0)
     x = _x(rng, N if gather else S, K, dtype, False, K + 3, 1)
     x64 = x.double().cpu().numpy()
     rows = x64[src // k] if gather else x64
