@@ -73,7 +73,11 @@ struct Tile {
 // correction, -(BASE + zero) * (sum of x), is one more matrix instruction: the
 // sum of x is found when x is staged and lies behind its row in three parts, whose
 // sum is exact, and the other operand is -(BASE + zero) three times.
-template <int DT, int NT, bool WHOLE, bool ZEROS>
+//
+// WORDS: rows of codes begin at multiples of 4 bytes.  Others are loaded from the
+// multiple of 4 below and shifted in registers (32768 rows on 64 experts of 4096 x
+// 2044, rows of 1022 bytes: 1241 us loaded at their own addresses, 904 us shifted).
+template <int DT, int NT, bool WHOLE, bool ZEROS, bool WORDS>
 __global__ __launch_bounds__(kThreads, 2) void q4_tile_kernel(const Q4Args a) {
   typedef Tile<DT, NT, WHOLE> C;
   typedef Type<DT> T;
@@ -102,7 +106,7 @@ __global__ __launch_bounds__(kThreads, 2) void q4_tile_kernel(const Q4Args a) {
   const uint8_t* codes[kB];
   const char* scales[kB];
   const uint8_t* zeros[kB];
-  uint32_t codes_at[kB], group_at[kB];
+  uint32_t codes_at[kB], group_at[kB], shift[kB];
 #pragma unroll
   for (int b = 0; b < kB; ++b) {
     const int64_t from = m0 + (pair == 2 ? 0 : 32 * b);  // may lie behind the last row: then all lanes take that one
@@ -114,6 +118,13 @@ __global__ __launch_bounds__(kThreads, 2) void q4_tile_kernel(const Q4Args a) {
     scales[b] = a.scales + row * a.groups * 2;
     zeros[b] = a.zeros ? a.zeros + row * a.groups : nullptr;
     codes_at[b] = (uint32_t)(m - base) * (uint32_t)a.row_bytes + half * 16;
+    if (!WORDS) {
+      const uint32_t off = (uint32_t)(reinterpret_cast<uintptr_t>(codes[b]) & 3);
+      codes[b] -= off;
+      codes_at[b] += off;
+      shift[b] = codes_at[b] & 3;
+      codes_at[b] -= shift[b];
+    }
     group_at[b] = (uint32_t)(m - base) * (uint32_t)a.groups;
   }
   // Staging: thread (row, chunk) has vector `chunk` of rows row, row + 16, ...
@@ -132,6 +143,7 @@ __global__ __launch_bounds__(kThreads, 2) void q4_tile_kernel(const Q4Args a) {
     vec16 w[kB][2];  // bytes half * 16 .. of each 32: word j has columns 64 i + 32 half + 8 j
     typename T::elt scale[kB][C::GROUPS];
     uint32_t zero[kB][C::GROUPS];
+    uint32_t behind[kB];  // not WORDS: the word behind the row's last one here
   };
   // tail: the step passes the end of K.
   auto load_weights = [&](Weights& o, int step, bool tail) {
@@ -140,8 +152,18 @@ __global__ __launch_bounds__(kThreads, 2) void q4_tile_kernel(const Q4Args a) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const uint8_t* base = codes[b] + (int64_t)step * (kStep / 2) + 32 * i;
-        o.w[b][i] = tail ? load_codes_end(a, base + codes_at[b]) : load16(reinterpret_cast<const char*>(base) + codes_at[b]);
+        o.w[b][i] = !tail   ? load16(reinterpret_cast<const char*>(base) + codes_at[b])
+                    : WORDS ? load_codes_end(a, base + codes_at[b])
+                            : load_words_end(a, base + codes_at[b]);
       }
+    if (!WORDS) {
+#pragma unroll
+      for (int b = 0; b < kB; ++b) {  // a row on a multiple of 4 needs no word behind
+        const uint8_t* p = codes[b] + (int64_t)step * (kStep / 2) + codes_at[b] + (64 - 16 * half - (shift[b] ? 0 : 4));
+        if (tail && p >= a.codes + a.codes_bytes) p = codes[b] + codes_at[b];  // not used: any word of the row
+        o.behind[b] = *reinterpret_cast<const uint32_t*>(p);
+      }
+    }
 #pragma unroll
     for (int g = 0; g < C::GROUPS; ++g) {
       uint32_t at = divide_by(a.by_group_blocks, (uint32_t)(step * 4 + g));
@@ -195,9 +217,22 @@ __global__ __launch_bounds__(kThreads, 2) void q4_tile_kernel(const Q4Args a) {
     if (after != NONE) {
       load_weights(next, step + 1, after == TAIL_STEP);
       load_rows(staged, step + 1, after == TAIL_STEP);
-
     }
     const char* from = lds[step & 1] + r32 * C::PITCH;
+    if (!WORDS) {
+      // The word after a lane's four: the other half's first one, of the same 32 bytes or of the next.
+#pragma unroll
+      for (int b = 0; b < kB; ++b) {
+        const u32x2 both = __builtin_amdgcn_permlane32_swap(now.w[b][0][0], now.w[b][1][0], false, false);
+        const u32x2 upper = __builtin_amdgcn_permlane32_swap(now.w[b][1][0], now.w[b][1][0], false, false);
+        const uint32_t after[2] = {half ? both[0] : both[1], half ? now.behind[b] : upper[1]};
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            now.w[b][i][j] = __builtin_amdgcn_alignbyte(j < 3 ? now.w[b][i][j < 3 ? j + 1 : 3] : after[i], now.w[b][i][j], shift[b]);
+      }
+    }
 #pragma unroll
     for (int b = 0; b < kB; ++b)
 #pragma unroll
@@ -281,18 +316,21 @@ __global__ __launch_bounds__(kThreads, 2) void q4_tile_kernel(const Q4Args a) {
 
 typedef void (*tile_fn)(const Q4Args);
 
-template <int DT>
+template <int DT, bool WORDS>
 tile_fn pick(int x_tiles, bool whole, bool zeros) {
-  if (!whole) return zeros ? q4_tile_kernel<DT, 2, false, true> : q4_tile_kernel<DT, 2, false, false>;
-  if (x_tiles == 1) return zeros ? q4_tile_kernel<DT, 1, true, true> : q4_tile_kernel<DT, 1, true, false>;
-  return zeros ? q4_tile_kernel<DT, 2, true, true> : q4_tile_kernel<DT, 2, true, false>;
+  if (!whole) return zeros ? q4_tile_kernel<DT, 2, false, true, WORDS> : q4_tile_kernel<DT, 2, false, false, WORDS>;
+  if (x_tiles == 1) return zeros ? q4_tile_kernel<DT, 1, true, true, WORDS> : q4_tile_kernel<DT, 1, true, false, WORDS>;
+  return zeros ? q4_tile_kernel<DT, 2, true, true, WORDS> : q4_tile_kernel<DT, 2, true, false, WORDS>;
 }
 
 }  // namespace
 
 void launch_q4_tile(const Q4Args& a, int dtype, int x_tiles, unsigned grid, hipStream_t stream) {
   const bool whole = a.group % 128 == 0;
-  const tile_fn fn = dtype == EBAG_F16 ? pick<1>(x_tiles, whole, a.zeros) : pick<2>(x_tiles, whole, a.zeros);
+  const bool words = a.row_bytes % 4 == 0 && reinterpret_cast<uintptr_t>(a.codes) % 4 == 0;
+  const tile_fn fn = dtype == EBAG_F16 ? words ? pick<1, true>(x_tiles, whole, a.zeros) : pick<1, false>(x_tiles, whole, a.zeros)
+                     : words           ? pick<2, true>(x_tiles, whole, a.zeros)
+                                       : pick<2, false>(x_tiles, whole, a.zeros);
   hipLaunchKernelGGL(fn, dim3(grid), dim3(kThreads), 0, stream, a);
 }
 
