@@ -64,7 +64,7 @@ __global__ __launch_bounds__(256) void q4_quantize_kernel(const QuantArgs a) {
   }
 }
 
-constexpr int kCuLds = 160 * 1024;
+constexpr int kCuLds = 160 * 1024, kCus = 256;
 
 int hipf(hipError_t e, const char* what) { return fail(EBAG_EHIP, "%s: %s", what, hipGetErrorString(e)); }
 
@@ -164,16 +164,25 @@ int launch_few(const gemv_ar_q4_plan* h, Q4Args a, hipStream_t stream) {
   const int64_t tiles = (all_turns + turns - 1) / turns;
   if (tiles * slots > INT_MAX) return fail(EBAG_EUNSUPPORTED, "too many tiles for one launch");
   a.by_tiles = make_divisor(tiles);
-  // LDS for x: 40 KiB, or a turn's columns of 16 rows where they are more.
-  const int64_t least = (int64_t)rows * parts * (2 * a.split * columns + 16);
-  const int64_t room = least > 40960 ? least : 40960;
+  // LDS for x: all of it up to 40 KiB; or what as many workgroups as a CU gets, or as its registers hold, leave each
+  // other; a turn's columns at least (12 x 10000 x 4992 on 625 workgroups: 20.9 us with 49 KB each, 26.8 with 61, 38 with
+  // 88; one fp32 row x 4096 x 11008 on 256: all of x at once 14.5 us, 40 KB at a time 19.1; 2 x 65536 x 8192, 33 KB of x:
+  // three workgroups on a CU 66 us, four that stage x anew for every tile 78).
   a.all_columns = units * columns;
+  const int64_t all_x = (int64_t)rows * parts * (2 * (int64_t)a.all_columns + 16);
+  const int64_t least = (int64_t)rows * parts * (2 * a.split * columns + 16);
+  const int64_t held = (rt == 2 ? 8 : 16) / waves, each = (tiles * slots + kCus - 1) / kCus, on_cu = each < held ? each : held;
+  int64_t room = kCuLds / on_cu - (a.split > 1 ? sums : 0) - 16;
+  if (room < all_x && all_x <= 40960) room = all_x;
+  if (room < least) room = least;
   const int64_t fit = room / (parts * (2 * (int64_t)a.all_columns + 16));
   a.fit_rows = fit < rows ? (int)fit : rows;
   a.some_columns = (int)((room / (rows * parts) - 16) / (2 * a.split * columns)) * a.split * columns;
   a.by_all = make_divisor(a.all_columns / 8);
   a.by_some = make_divisor(a.some_columns / 8);
-  a.x_bytes = (int)(a.fit_rows < rows ? (room + 15) / 16 * 16 : rows * parts * (2 * (int64_t)a.all_columns + 16));
+  const int64_t all = a.fit_rows * parts * (2 * (int64_t)a.all_columns + 16);
+  const int64_t some = a.fit_rows < rows ? rows * parts * (2 * (int64_t)a.some_columns + 16) : 0;
+  a.x_bytes = (int)(all > some ? all : some);
   const size_t lds = a.x_bytes + (a.split > 1 ? sums : 0);
   const Q4FewKind kind = {rt, whole, a.zeros != nullptr, a.row_bytes % 4 == 0 && reinterpret_cast<uintptr_t>(a.codes) % 4 == 0};
   const q4_fn fn = h->dtype == EBAG_F32 ? pick_q4_few_f32(kind) : h->dtype == EBAG_F16 ? pick_q4_few_f16(kind) : pick_q4_few_bf16(kind);

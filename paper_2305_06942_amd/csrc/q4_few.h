@@ -339,75 +339,54 @@ __global__ __launch_bounds__(kFewThreads, C::RT == 1 ? 4 : 2) void q4_few_kernel
       load_weights<true>(a, f, o);
   };
 
-  if (fits) {
-    // Two units in turn through all turns: each is loaded while the other one is worked on.
-    start(m0);
-    load(even);
-    stage_x<DT>(a, first, rows, 0, a.by_all, pitch, lds);
+  // x: all columns once, or the part that has a unit, for every tile anew.  All of a tile's waves come here as often.
+  int from_unit = 0, to_unit = 0;
+  auto stage = [&]() {
+    from_unit = to_unit;
+    to_unit = fits ? units : from_unit + columns / C::COLUMNS;
     __syncthreads();
-    bool more, ends;
-    int now;
-    auto next = [&]() {
-      now = f.unit;
-      f.advance();
-      ends = f.unit >= units;
-      more = !ends || turn + 1 < turns;
-      if (ends && more) start(m0 + turn_rows);
-    };
-    for (;;) {
-      next();
-      if (!more) {
-        times(even, now);
-        break;
-      }
-      load(odd);
-      times(even, now);
-      if (ends) finish();
-      next();
-      if (!more) {
-        times(odd, now);
-        break;
-      }
-      load(even);
-      times(odd, now);
-      if (ends) finish();
+    stage_x<DT>(a, first, rows, from_unit * C::COLUMNS, fits ? a.by_all : a.by_some, pitch, lds);
+    __syncthreads();
+  };
+  // Two units in turn through all turns: each is loaded while the other one is worked on.
+  start(m0);
+  load(even);
+  bool more, ends;
+  int now;
+  auto next = [&]() {
+    now = f.unit;
+    if (now >= to_unit) stage();
+    f.advance();
+    ends = f.unit >= units;
+    more = !ends || turn + 1 < turns;
+    if (ends && more) start(m0 + turn_rows);
+  };
+  auto end_tile = [&]() {
+    if (!fits) {
+      while (to_unit < units) stage();
+      to_unit = 0;
     }
     finish();
-    return;
-  }
-  // Part of the columns of x at a time: a tile's units among them, then the next part.
-  for (int t = 0; t < turns; ++t) {
-    start(m0);
-    for (int k0 = 0; k0 < a.K; k0 += columns) {
-      const int first_unit = k0 / C::COLUMNS, end_unit = first_unit + columns / C::COLUMNS;
-      const int last = end_unit < units ? end_unit : units;
-      if (f.unit < last) load(even);
-      if (t || k0) __syncthreads();
-      stage_x<DT>(a, first, rows, k0, a.by_some, pitch, lds);
-      __syncthreads();
-      if (f.unit < last) {
-        for (;;) {
-          int now = f.unit;
-          f.advance();
-          if (f.unit >= last) {
-            times(even, now - first_unit);
-            break;
-          }
-          load(odd);
-          times(even, now - first_unit);
-          now = f.unit;
-          f.advance();
-          if (f.unit >= last) {
-            times(odd, now - first_unit);
-            break;
-          }
-          load(even);
-          times(odd, now - first_unit);
-        }
-      }
+  };
+  for (;;) {
+    next();
+    if (!more) {
+      times(even, now - from_unit);
+      break;
     }
-    finish();
+    load(odd);
+    times(even, now - from_unit);
+    if (ends) end_tile();
+    next();
+    if (!more) {
+      times(odd, now - from_unit);
+      break;
+    }
+    load(even);
+    times(odd, now - from_unit);
+    if (ends) end_tile();
   }
+  end_tile();
 }
 
 // The instance for a launch.
