@@ -49,10 +49,11 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 // bit pattern away in fp16 and bf16 (BASE is a power of two with q at the bottom
 // of its mantissa, or above it) and exact; BASE and the zero point come off again
 // as (BASE + zero) * (the sum of x over the group).  The sums grow by BASE / 8 at
-// most that way, so fp32 loses 3 bits (fp16), 4 (bf16) or 1 (fp32) of its 24: the
-// larger BASE leaves one code of four where it is and saves its shift.  fp32 x
-// goes as three bf16 parts whose sum is x, bit for bit, so its products are exact
-// too.
+// most that way, so fp32 loses 3 bits (fp16) or 4 (bf16) of its 24: fewer than the
+// results' rounding to 11 and 8 bits does, and the larger BASE leaves one code of
+// four where it is and saves its shift.  fp32 x goes as three bf16 parts whose sum
+// is x, bit for bit, so its products are exact too; its results keep all their bits,
+// so there BASE + zero comes off each code before the products (`centred`).
 template <int DT> struct Q4Type;
 
 template <> struct Q4Type<1> {
@@ -80,19 +81,21 @@ template <> struct Q4Type<2> {
 
 template <> struct Q4Type<0> : Q4Type<2> {
   static constexpr int PARTS = 3;
-  static constexpr float BASE = 16.f;
-  static constexpr uint32_t MASK = 0x00780078u, HIGH = 0x41804180u;
-  static __device__ __forceinline__ uint32_t pair(uint32_t w, int j) { return j == 0 ? w << 3 : w >> (4 * j - 3); }
 };
 
 // MASK and HIGH in registers: as literals they would take an instruction each,
-// and from one scalar and one vector register both go into one.
+// and from one scalar and one vector register both go into one.  fp32: 1 in the
+// lower and in the upper half, too (as an inline constant 1.0 stands in the upper one).
 template <int DT>
 struct CodeBits {
-  uint32_t mask, high;
+  uint32_t mask, high, lower, upper;
   __device__ __forceinline__ CodeBits() {
     asm volatile("s_mov_b32 %0, %1" : "=s"(mask) : "i"(Q4Type<DT>::MASK));
     asm volatile("v_mov_b32 %0, %1" : "=v"(high) : "i"(Q4Type<DT>::HIGH));
+    if (DT == 0) {
+      asm volatile("s_mov_b32 %0, 0x3f80" : "=s"(lower));
+      asm volatile("s_mov_b32 %0, 0x3f800000" : "=s"(upper));
+    }
   }
 };
 
@@ -102,6 +105,20 @@ __device__ __forceinline__ vec16 unpack_codes(const CodeBits<DT>& c, uint32_t w)
   vec16 r;
 #pragma unroll
   for (int j = 0; j < 4; ++j) r[j] = (Q4Type<DT>::pair(w, j) & c.mask) | c.high;
+  return r;
+}
+
+// Eight bf16 numbers BASE + q with off = -(BASE + zero) added: q - zero, exact.  A dot
+// product with (1, 0) or (0, 1) widens one of two and adds in one instruction.
+__device__ __forceinline__ vec16 centred(const CodeBits<0>& c, const vec16& codes, float off) {
+  vec16 r;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint32_t two = codes[j];
+    const float lo = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, c.lower), __builtin_bit_cast(bf16x2, two), off, false);
+    const float hi = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, c.upper), __builtin_bit_cast(bf16x2, two), off, false);
+    r[j] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
+  }
   return r;
 }
 

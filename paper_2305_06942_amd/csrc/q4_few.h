@@ -175,20 +175,19 @@ __device__ __forceinline__ void multiply(const CodeBits<C::DT>& bits, Unit<C>& o
       vec16 xs[PARTS];
 #pragma unroll
       for (int p = 0; p < PARTS; ++p) xs[p] = *reinterpret_cast<const vec16*>(x + p * pitch + (s * 4 + t) * 64);
-      if (!C::WHOLE || t == 0) xsum = f32x4{0, 0, 0, 0};
-#pragma unroll
-      for (int p = 0; p < PARTS; ++p) xsum = Q::mfma(xs[p], ones, xsum);
+      if (!F32) xsum = Q::mfma(xs[0], ones, C::WHOLE && t ? xsum : f32x4{0, 0, 0, 0});
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
-        const vec16 q = unpack_codes(bits, o.w[s][rt][t]);
+        const int g = C::WHOLE ? 0 : t;
+        vec16 q = unpack_codes(bits, o.w[s][rt][t]);
+        if constexpr (F32) q = centred(bits, q, off[rt][g]);
         if (!C::WHOLE || t == 0) v[rt] = f32x4{0, 0, 0, 0};
 #pragma unroll
         for (int p = 0; p < PARTS; ++p) v[rt] = Q::mfma(xs[p], q, v[rt]);
         if (C::WHOLE && t < 3) continue;
-        const int g = C::WHOLE ? 0 : t;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          sum[rt][i] = __builtin_fmaf(scale[rt][g], __builtin_fmaf(off[rt][g], xsum[i], v[rt][i]), sum[rt][i]);
+          sum[rt][i] = __builtin_fmaf(scale[rt][g], F32 ? v[rt][i] : __builtin_fmaf(off[rt][g], xsum[i], v[rt][i]), sum[rt][i]);
       }
     }
   }

@@ -3,14 +3,14 @@
 Exact inputs: whole x below 2^7, scales that are powers of two and sums below
 2^24 leave fp32 nothing to round, so such results are compared bit for bit.
 
-Others: with fp32 x a code goes through the sums as 16 + q (at most 31) and the
-zero's part comes off again, so fp32 sums terms of up to 62 s |x| in all.  The
-longest chain has 128 products of a group, a multiply-add pair per 32 columns
-and at most 16 partial sums; with 2^-23 for each (sums of a matrix instruction
-need not be rounded to nearest), |sum - want| <= b = (128 + K / 16 + 16) 2^-23 *
-62 sum_k s |x|.  With fp16 and bf16 x a code goes as 64 + q or 128 + q, terms of
-up to 286 s |x|, but a matrix instruction adds 32 columns: 512 columns are 16
-steps, and 16 * 286 < 128 * 62, so b holds there too.
+Others: let every term of a sum be at most 62 s |x| and the longest chain 128
+products of a group, a multiply-add pair per 32 columns and at most 16 partial
+sums; with 2^-23 for each (sums of a matrix instruction need not be rounded to
+nearest), |sum - want| <= b = (128 + K / 16 + 16) 2^-23 * 62 sum_k s |x|.  With
+fp32 x the terms are (q - zero) s x, at most 15 s |x|.  With fp16 and bf16 x a
+code goes as 64 + q or 128 + q, whose part comes off again: terms of up to 286 s
+|x|, but a matrix instruction adds 32 columns, 512 columns are 16 steps, and 16 *
+286 < 128 * 62.
 
 silu(g) = g / (1 + exp(-g)) with an exponential good to (|g| + 8) 2^-22 and a
 slope of at most 1.1 carries b on.  Rounding to the storage type keeps order, so
