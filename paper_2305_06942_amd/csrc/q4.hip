@@ -171,7 +171,7 @@ int launch_few(const gemv_ar_q4_plan* h, Q4Args a, hipStream_t stream) {
   a.all_columns = units * columns;
   const int64_t all_x = (int64_t)rows * parts * (2 * (int64_t)a.all_columns + 16);
   const int64_t least = (int64_t)rows * parts * (2 * a.split * columns + 16);
-  const int64_t held = (rt == 2 ? 8 : 16) / waves, each = (tiles * slots + kCus - 1) / kCus, on_cu = each < held ? each : held;
+  const int64_t held = (rt == 2 ? 8 : parts == 3 ? 12 : 16) / waves, each = (tiles * slots + kCus - 1) / kCus, on_cu = each < held ? each : held;
   int64_t room = kCuLds / on_cu - (a.split > 1 ? sums : 0) - 16;
   if (room < all_x && all_x <= 40960) room = all_x;
   if (room < least) room = least;

@@ -228,7 +228,7 @@ __device__ __forceinline__ void stage_x(const Q4Args& a, uint32_t first, int row
 }
 
 template <class C>
-__global__ __launch_bounds__(kFewThreads, C::RT == 1 ? 4 : 2) void q4_few_kernel(const Q4Args a) {
+__global__ __launch_bounds__(kFewThreads, C::RT == 2 ? 2 : C::DT == 0 ? 3 : 4) void q4_few_kernel(const Q4Args a) {
   constexpr int DT = C::DT, RT = C::RT;
   extern __shared__ __attribute__((aligned(16))) char lds[];  // x; the waves' sums [2][waves][RT][64]
   const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
