@@ -7,6 +7,7 @@
 
 #include "ebag_a2a.h"
 #include "gemv_ar.h"
+#include "lanes.h"
 #include "q4.h"
 
 using namespace ebag;
@@ -14,6 +15,8 @@ using namespace ebag;
 namespace {
 
 // ------------------------------------------------------------------- to 4 bits
+
+constexpr int kQuantThreads = 256;
 
 struct QuantArgs {
   const char* w;
@@ -23,44 +26,82 @@ struct QuantArgs {
   int64_t rows;  // of all matrices
   int64_t row_bytes;
   int32_t K, group, groups;
+  int32_t lanes;      // that share a group, 2^k <= 64
+  Divisor by_groups;
 };
 
-// A wave has a group of a row.
+// 2^k lanes have a group of a row, 8 columns each at a time: what a lane loads as
+// one vector (two in fp32) it stores as one word of codes.  Values of groups of up to
+// 512 columns stay in registers between the extremes and the codes.  65536 x 8192
+// bf16, groups of 128: 486 us, 2.8 TB/s read and written, bound by the eight exact
+// divisions of a lane.
 template <int DT>
-__global__ __launch_bounds__(256) void q4_quantize_kernel(const QuantArgs a) {
+__global__ __launch_bounds__(kQuantThreads) void q4_quantize_kernel(const QuantArgs a) {
   typedef Type<DT> T;
-  const int lane = threadIdx.x & 63;
-  const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (at >= a.rows * a.groups) return;
-  const int64_t row = at / a.groups;
-  const int k0 = (int)(at - row * a.groups) * a.group, k1 = a.K - k0 < a.group ? a.K : k0 + a.group;
-  const typename T::elt* w = reinterpret_cast<const typename T::elt*>(a.w) + row * a.K;
-  float lo = 0.f, hi = 0.f;
-  for (int k = k0 + lane; k < k1; k += 64) {
-    const float v = T::widen(w[k]);
-    lo = fminf(lo, v);
-    hi = fmaxf(hi, v);
+  typedef typename T::elt elt;
+  constexpr int VECS = 8 / T::N;
+  const int per_wg = kQuantThreads / a.lanes, own = threadIdx.x / a.lanes, lane = threadIdx.x % a.lanes;
+  const int64_t first = (int64_t)blockIdx.x * per_wg, first_row = first / a.groups;
+  const uint32_t g_on = (uint32_t)(first - first_row * a.groups) + own, rows_on = divide_by(a.by_groups, g_on);
+  const int64_t row = first_row + rows_on;
+  if (row >= a.rows) return;  // all lanes of a group together
+  const int64_t k0 = (int64_t)(g_on - rows_on * a.groups) * a.group;
+  const int64_t k1 = a.K - k0 < a.group ? a.K : k0 + a.group, step = 8 * a.lanes;
+  const char* w = a.w + row * a.K * (int64_t)sizeof(elt);
+  auto load = [&](float* f, int64_t k) {
+    if (k + 8 <= k1) {
+#pragma unroll
+      for (int i = 0; i < VECS; ++i) T::widen(load16(w + k * (int64_t)sizeof(elt) + 16 * i), f + i * T::N);
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = k + i < k1 ? T::widen(reinterpret_cast<const elt*>(w)[k + i]) : 0.f;
+  };
+  float hi = 0.f, minus_lo = 0.f;
+  auto extremes = [&](const float* f) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      hi = fmaxf(hi, f[i]);
+      minus_lo = fmaxf(minus_lo, -f[i]);
+    }
+  };
+  const int64_t k = k0 + 8 * lane;
+  float mine[8], more[8];
+  load(mine, k);
+  extremes(mine);
+  for (int64_t at = k + step; at < k1; at += step) {
+    load(more, at);
+    extremes(more);
   }
-  for (int d = 32; d; d /= 2) {
-    lo = fminf(lo, __shfl_xor(lo, d));
-    hi = fmaxf(hi, __shfl_xor(hi, d));
-  }
-  const typename T::elt scale = T::narrow(a.zeros ? (hi - lo) / 15.f : fmaxf(hi, -lo) / 7.f);
+  hi = max_lanes(hi, a.lanes);
+  minus_lo = max_lanes(minus_lo, a.lanes);
+  const elt scale = T::narrow(a.zeros ? (hi + minus_lo) / 15.f : fmaxf(hi, minus_lo) / 7.f);
   const float s = T::widen(scale);
   float zero = 8.f;
-  if (a.zeros) zero = s > 0.f ? fminf(fmaxf(rintf(-lo / s), 0.f), 15.f) : 0.f;
+  if (a.zeros) zero = s > 0.f ? fminf(fmaxf(rintf(minus_lo / s), 0.f), 15.f) : 0.f;
   if (lane == 0) {
-    reinterpret_cast<typename T::elt*>(a.scales)[at] = scale;
+    const int64_t at = row * a.groups + (g_on - rows_on * a.groups);
+    reinterpret_cast<elt*>(a.scales)[at] = scale;
     if (a.zeros) a.zeros[at] = (uint8_t)zero;
   }
-  uint8_t* out = a.codes + row * a.row_bytes;
-  for (int k = k0 + 2 * lane; k < k1; k += 128) {  // a byte: groups begin at even columns
-    uint32_t byte = 0;
-    for (int i = 0; i < 2 && k + i < k1; ++i) {
-      const float q = s > 0.f ? rintf(T::widen(w[k + i]) / s) + zero : zero;
-      byte |= (uint32_t)fminf(fmaxf(q, 0.f), 15.f) << (4 * i);
+  auto store = [&](const float* f, int64_t at) {
+    const int have = k1 - at < 8 ? (int)(k1 - at) : 8;
+    uint32_t word = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float q = s > 0.f ? rintf(f[i] / s) + zero : zero;
+      word |= i < have ? (uint32_t)fminf(fmaxf(q, 0.f), 15.f) << (4 * i) : 0u;
     }
-    out[k / 2] = (uint8_t)byte;
+    uint8_t* out = a.codes + row * a.row_bytes + at / 2;  // groups begin at even columns
+    if (have == 8)
+      __builtin_memcpy(out, &word, 4);
+    else
+      for (int i = 0; 2 * i < have; ++i) out[i] = (uint8_t)(word >> (8 * i));
+  };
+  if (k < k1) store(mine, k);
+  for (int64_t at = k + step; at < k1; at += step) {
+    load(more, at);
+    store(more, at);
   }
 }
 
@@ -278,12 +319,15 @@ int gemv_ar_q4_quantize(gemv_ar_q4_t h, const void* w, uint8_t* codes, void* sca
   a.K = (int32_t)h->K;
   a.group = h->group;
   a.groups = (int32_t)((h->K + h->group - 1) / h->group);
-  const int64_t wgs = (a.rows * a.groups + 3) / 4;
+  a.by_groups = make_divisor(a.groups);
+  a.lanes = 1;
+  while (a.lanes < 64 && 8 * a.lanes < a.group) a.lanes *= 2;
+  const int64_t per_wg = kQuantThreads / a.lanes, wgs = (a.rows * a.groups + per_wg - 1) / per_wg;
   if (wgs > INT_MAX) return fail(EBAG_EUNSUPPORTED, "too many groups for one launch");
   void (*fn)(const QuantArgs) = h->dtype == EBAG_F32   ? q4_quantize_kernel<0>
                                 : h->dtype == EBAG_F16 ? q4_quantize_kernel<1>
                                                        : q4_quantize_kernel<2>;
-  hipLaunchKernelGGL(fn, dim3((unsigned)wgs), dim3(256), 0, stream, a);
+  hipLaunchKernelGGL(fn, dim3((unsigned)wgs), dim3(kQuantThreads), 0, stream, a);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? EBAG_OK : hipf(e, "launch the rounding to 4 bits");
 }

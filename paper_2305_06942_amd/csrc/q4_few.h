@@ -12,19 +12,30 @@
 namespace ebag {
 namespace {
 
-// A workgroup has RT tiles of 16 rows of weights and 16 rows of x; its
-// waves split K in units of 256 columns (a cache line of codes), wave w
-// taking units w, w + waves, ..., and join their sums in LDS at the end.  A
-// lane loads 16 bytes, 32 consecutive codes of row lane % 16; a transposition
-// between the four lanes of a row (lane / 16) then gives word t of each the
-// columns 32 t + 8 (lane / 16) .. + 8, the layout of a 16x16x32 matrix
-// instruction over 32 consecutive columns, which belong to one group.  x is
-// the first operand, so a lane holds sums of ONE weight row for four rows of x
-// and needs one scale per group: the four lanes of a row load those of four
-// blocks of 32 columns and pass them round.  Rows of a tile beyond the last one
-// repeat it; nothing they give is stored.
+// A tile is 16 rows of weights (RT = 2 with glu: 16 gate rows and the up rows that go
+// with them) and up to 16 rows of x; `split` waves share one, each taking every
+// split-th unit of 512 or 256 columns (256 or 128 bytes of codes), and join their sums
+// in LDS at the end.  A workgroup has 4 or 8 waves on one tile or several and goes on
+// to the tiles of `turns` more rows of weights with the same x in LDS.  A lane loads
+// 16 bytes, 32 consecutive codes of row lane % 16; a transposition between the four
+// lanes of a row (lane / 16) then gives word t of each the columns 32 t + 8 (lane / 16)
+// .. + 8, the layout of a 16x16x32 matrix instruction over 32 consecutive columns,
+// which belong to one group.  x is the first operand, so a lane holds sums of ONE
+// weight row for four rows of x and needs one scale per group: the four lanes of a row
+// load those of four blocks of 32 columns (or of four steps, where a group is several
+// blocks) and pass them round.  Rows of a tile beyond the last one repeat it; nothing
+// they give is stored.
 //
 // The loads of a wave's next unit are under way while it works on one.
+//
+// Bound by the codes' bytes with one to four rows: 65536 x 8192 fp16, one row, 277 MB
+// in 56 us, 4.9 TB/s (this pattern of 16 rows a wave reads 5.3 to 5.5 and a plain
+// stream 6.5; two thirds of the rest are the scales' loads); 128 experts of 2 x 1024 x
+// 2048, two rows each, 246 MB in 61 us.  A launch of a few MB is bound by its chain of
+// launch, x, codes, join and store: 4096 x 4096, one row, 5.5 us.  Many rows of x, or
+// scales for every 32 columns, bound it by the instructions of a block of 32 columns
+// (22 of the vector unit, 2 of the matrix unit) and by staging x: 12 x 10001 x 5001
+// 26 us, 60 experts of 1400 x 1000 with 20 rows each 28 us.
 
 // Between lanes l, l + 16, l + 32, l + 48: w[t] of lane quarter c becomes w[c] of quarter t.
 __device__ __forceinline__ void transpose_words(vec16& w) {

@@ -307,7 +307,8 @@ def test_fp32_counts_with_all_its_bits():
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("zeros", [False, True])
-@pytest.mark.parametrize("E,M,K,group", [(1, 3, 1, 32), (2, 5, 100, 32), (1, 7, 257, 96), (3, 16, 512, 128), (1, 2, 333, 1024)])
+@pytest.mark.parametrize("E,M,K,group", [(1, 3, 1, 32), (2, 5, 100, 32), (1, 7, 257, 96), (3, 16, 512, 128), (1, 2, 333, 1024),
+                                          (1, 41, 1000, 64), (2, 9, 769, 256), (1, 3, 2500, 1024)])
 def test_quantize(E, M, K, group, zeros, dtype):
     import torch
     import paper_2305_06942_amd as ebag
