@@ -281,9 +281,9 @@ q4_fn pick_q4_few_f32(const Q4FewKind& k);
 q4_fn pick_q4_few_f16(const Q4FewKind& k);
 q4_fn pick_q4_few_bf16(const Q4FewKind& k);
 
-// The matrix-product kernel for many rows of fp16 or bf16 x: a workgroup for
+// The matrix-product kernel for many rows of x: a workgroup for
 // kQ4TileRows rows of weights (half as many outputs with glu) and 32 x_tiles (1 or
-// 2) rows of x.
+// 2; fp32: 1) rows of x.
 constexpr int kQ4TileRows = 256;
 void launch_q4_tile(const Q4Args& a, int dtype, int x_tiles, unsigned grid, hipStream_t stream);
 

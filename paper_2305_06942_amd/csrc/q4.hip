@@ -250,9 +250,11 @@ int launch_tile(const gemv_ar_q4_plan* h, Q4Args a, int x_tiles, hipStream_t str
 // time.  Where a step of 128 columns has several scales: 12.5 ns, and with 64 rows 480
 // ns and 107 us.  (64 experts of 4096 x 2048, in us by the three: 12 rows each 94, 89, 101; 48
 // rows 280, 141, 129.  One matrix of 8192 x 4096: 64 rows 22, 48, 67; 256 rows 64, 49,
-// 67.)  An expert's rows fill their last tile half on average.
+// 67.)  fp32 x: 16.5 ns; with 32 rows 235 ns and 64 us, or 272 ns and 85 us (one of 4096 x
+// 4096, in us by the two: 64 rows 34, 63; 512 rows 128, 69; 2048 rows 490, 234; with groups
+// of 32 523, 279).  An expert's rows fill their last tile half on average.
 int launch(const gemv_ar_q4_plan* h, const Q4Args& a, hipStream_t stream) {
-  if (h->dtype == EBAG_F32 || h->K >= 1 << 27) return launch_few(h, a, stream);
+  if (h->K >= 1 << 27) return launch_few(h, a, stream);
   const bool whole = h->group % 128 == 0;
   auto tiles = [&](double rows, double cols) {  // of `rows` weight rows and `cols` rows of x
     const double experts = a.offsets ? h->experts : 1, some = a.rows < experts ? a.rows : experts;
@@ -261,6 +263,10 @@ int launch(const gemv_ar_q4_plan* h, const Q4Args& a, hipStream_t stream) {
     return (double)((h->M + (int)rows - 1) / (int)rows) * (n < a.rows ? n : a.rows);
   };
   auto at_least = [](double v, double least) { return v < least ? least : v; };
+  if (h->dtype == EBAG_F32) {
+    const double tile = at_least(tiles(kQ4TileRows, 32) * (whole ? 0.235 : 0.272), whole ? 64 : 85);
+    return tiles(16, 16) * 0.0165 <= tile ? launch_few(h, a, stream) : launch_tile(h, a, 1, stream);
+  }
   const double few = tiles(16, 16) * (whole ? 0.0080 : 0.0125);
   const double one = at_least(tiles(kQ4TileRows, 32) * 0.157, 45);
   const double two = at_least(tiles(kQ4TileRows, 64) * (whole ? 0.203 : 0.48), whole ? 62 : 107);

@@ -54,13 +54,15 @@ __device__ __forceinline__ vec16 three_parts(float f) {
 }
 
 // WHOLE: a group is a multiple of 128 columns, so a step has one scale; otherwise
-// every block of 32 columns has its own (only with 64 rows of x: with 32 the kernel
-// for few rows is never slower).
+// every block of 32 columns has its own (fp16 and bf16: only with 64 rows of x, as with
+// 32 the kernel for few rows is never slower; fp32: only 32, whose three parts fill LDS).
 template <int DT, int NT, bool WHOLE>
 struct Tile {
   static constexpr int BN = 32 * NT;                  // rows of x
   static constexpr int GROUPS = WHOLE ? 1 : 4;        // of a step
-  static constexpr int PITCH = WHOLE ? 272 : 336;     // bytes of a row of x in LDS: 16 lanes' vectors on different banks
+  static constexpr int PARTS = Q4Type<DT>::PARTS, VECS = DT == 0 ? 2 : 1, ELT = sizeof(typename Type<DT>::elt);
+  static constexpr int PITCH = DT == 0 || WHOLE ? 272 : 336;  // bytes of a row of x in LDS: 16 lanes' vectors on different banks
+  static constexpr int PART = BN * PITCH;             // of one part of fp32 x
   static constexpr int STAGED = BN * 16 / kThreads;   // vectors of a thread
 };
 
@@ -72,7 +74,9 @@ struct Tile {
 // and the zero point, and are added to the tile's sums times the scale.  The
 // correction, -(BASE + zero) * (sum of x), is one more matrix instruction: the
 // sum of x is found when x is staged and lies behind its row in three parts, whose
-// sum is exact, and the other operand is -(BASE + zero) three times.
+// sum is exact, and the other operand is -(BASE + zero) three times.  With fp32 x BASE
+// and zero come off the codes, and three parts of x are multiplied with them (2048 x
+// 4096 x 4096: 234 us, 294 TFLOP/s, 880 of the matrix unit's; fp32's own 154).
 //
 // Bound by the latency and the L1 work of its loads: 32768 rows on 64 experts of 4096 x
 // 2048 (550 GFLOP) 710 to 750 us, 750 TFLOP/s; a large bf16 product reaches 1360.  The
@@ -89,7 +93,7 @@ __global__ __launch_bounds__(kThreads, 2) void q4_tile_kernel(const Q4Args a) {
   typedef Tile<DT, NT, WHOLE> C;
   typedef Type<DT> T;
   typedef Q4Type<DT> Q;
-  __shared__ __attribute__((aligned(16))) char lds[2][C::BN * C::PITCH];
+  __shared__ __attribute__((aligned(16))) char lds[2][C::PARTS * C::PART];
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, r32 = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const uint32_t slot = divide_by(a.by_tiles, blockIdx.x), tile = blockIdx.x - slot * a.by_tiles.d;
@@ -122,7 +126,7 @@ __global__ __launch_bounds__(kThreads, 2) void q4_tile_kernel(const Q4Args a) {
     m = m < a.out_rows ? m : a.out_rows - 1;
     const int64_t row = base + (pair == 2 && b ? a.out_rows : 0) + (int64_t)expert * a.M;
     codes[b] = a.codes + row * a.row_bytes;
-    scales[b] = a.scales + row * a.groups * 2;
+    scales[b] = a.scales + row * a.groups * C::ELT;
     zeros[b] = a.zeros ? a.zeros + row * a.groups : nullptr;
     codes_at[b] = (uint32_t)(m - base) * (uint32_t)a.row_bytes + half * 16;
     if (!WORDS) {
@@ -143,7 +147,7 @@ __global__ __launch_bounds__(kThreads, 2) void q4_tile_kernel(const Q4Args a) {
     n = n < end ? n : end - 1;
     int64_t row = a.src ? (int64_t)divide_by(a.by_choices, (uint32_t)a.src[n] & 0x7fffffffu) : (int64_t)n;
     row = row < a.x_rows ? row : a.x_rows - 1;
-    x[i] = a.x + row * a.ldx + chunk * 16;
+    x[i] = a.x + row * a.ldx + chunk * (8 * C::ELT);
   }
 
   struct Weights {
@@ -177,34 +181,47 @@ __global__ __launch_bounds__(kThreads, 2) void q4_tile_kernel(const Q4Args a) {
       if (tail) at = at < (uint32_t)a.groups ? at : a.groups - 1;
 #pragma unroll
       for (int b = 0; b < kB; ++b) {
-        o.scale[b][g] = *reinterpret_cast<const typename T::elt*>(scales[b] + 2 * at + 2 * group_at[b]);
+        o.scale[b][g] = *reinterpret_cast<const typename T::elt*>(scales[b] + C::ELT * at + C::ELT * group_at[b]);
         o.zero[b][g] = ZEROS ? *(zeros[b] + at + group_at[b]) : 8u;
       }
     }
   };
-  auto load_rows = [&](vec16* v, int step, bool tail) {
+  auto load_rows = [&](vec16 (*v)[C::VECS], int step, bool tail) {
     if (!tail) {
 #pragma unroll
-      for (int i = 0; i < C::STAGED; ++i) v[i] = load16(x[i] + (int64_t)step * (kStep * 2));
+      for (int i = 0; i < C::STAGED; ++i)
+#pragma unroll
+        for (int j = 0; j < C::VECS; ++j) v[i][j] = load16(x[i] + (int64_t)step * (kStep * C::ELT) + 16 * j);
       return;
     }
     const int n = a.K - step * kStep - 8 * chunk;  // elements left
 #pragma unroll
-    for (int i = 0; i < C::STAGED; ++i) load_x<DT>(x[i] + (int64_t)step * (kStep * 2), n, a.K, &v[i]);
+    for (int i = 0; i < C::STAGED; ++i) load_x<DT>(x[i] + (int64_t)step * (kStep * C::ELT), n, a.K, v[i]);
   };
-  auto store_rows = [&](const vec16* v, char* to) {
-    // Lane `chunk` of a row (or of a quarter of it) finishes the sums of row number `chunk` % STAGED.
-    float mine = 0.f;
-    const int pick = (WHOLE ? chunk : chunk & 3) % C::STAGED;
+  auto store_rows = [&](const vec16 (*v)[C::VECS], char* to) {
     char* row = to + (tid >> 4) * C::PITCH;
+    if constexpr (DT == 0) {
 #pragma unroll
-    for (int i = 0; i < C::STAGED; ++i) {
-      const float s = sum_lanes(sum8<DT>(v[i]), WHOLE ? 16 : 4);
-      mine = i == pick ? s : mine;
-      *reinterpret_cast<vec16*>(row + 16 * i * C::PITCH + chunk * 16) = pair_order(v[i]);
+      for (int i = 0; i < C::STAGED; ++i) {
+        vec16 parts[C::PARTS];
+        split_f32(v[i][0], v[i][1], parts);
+#pragma unroll
+        for (int p = 0; p < C::PARTS; ++p)
+          *reinterpret_cast<vec16*>(row + p * C::PART + 16 * i * C::PITCH + chunk * 16) = parts[p];
+      }
+    } else {
+      // Lane `chunk` of a row (or of a quarter of it) finishes the sums of row number `chunk` % STAGED.
+      float mine = 0.f;
+      const int pick = (WHOLE ? chunk : chunk & 3) % C::STAGED;
+#pragma unroll
+      for (int i = 0; i < C::STAGED; ++i) {
+        const float s = sum_lanes(sum8<DT>(v[i][0]), WHOLE ? 16 : 4);
+        mine = i == pick ? s : mine;
+        *reinterpret_cast<vec16*>(row + 16 * i * C::PITCH + chunk * 16) = pair_order(v[i][0]);
+      }
+      if ((WHOLE ? chunk : chunk & 3) < C::STAGED)
+        *reinterpret_cast<vec16*>(row + 16 * pick * C::PITCH + 256 + (WHOLE ? 0 : chunk / 4 * 16)) = three_parts<DT>(mine);
     }
-    if ((WHOLE ? chunk : chunk & 3) < C::STAGED)
-      *reinterpret_cast<vec16*>(row + 16 * pick * C::PITCH + 256 + (WHOLE ? 0 : chunk / 4 * 16)) = three_parts<DT>(mine);
   };
 
   const CodeBits<DT> bits;
@@ -217,7 +234,7 @@ __global__ __launch_bounds__(kThreads, 2) void q4_tile_kernel(const Q4Args a) {
       for (int i = 0; i < 16; ++i) sum[b][t][i] = 0.f;
 
   Weights now, next;
-  vec16 staged[C::STAGED];
+  vec16 staged[C::STAGED][C::VECS];
   enum Next { WHOLE_STEP, TAIL_STEP, NONE };
   // One step's products; what the next one needs is loaded ahead of them and staged behind.
   auto work = [&](int step, Next after) __attribute__((always_inline)) {
@@ -257,36 +274,45 @@ __global__ __launch_bounds__(kThreads, 2) void q4_tile_kernel(const Q4Args a) {
 #pragma unroll
       for (int sl = 0; sl < SLICES; ++sl) {
         const int slice = g * SLICES + sl;
-        vec16 xs[NT];
+        vec16 xs[NT][C::PARTS];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) xs[t] = *reinterpret_cast<const vec16*>(from + 32 * t * C::PITCH + slice * 32 + half * 16);
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int p = 0; p < C::PARTS; ++p)
+            xs[t][p] = *reinterpret_cast<const vec16*>(from + p * C::PART + 32 * t * C::PITCH + slice * 32 + half * 16);
 #pragma unroll
         for (int b = 0; b < kB; ++b) {
           // Of each 64 columns, words 0 and 2 have the first 32, words 1 and 3 the others.
-          const vec16 q = unpack_codes(bits, now.w[b][slice / 4][slice % 4 / 2 + 2 * (slice % 2)]);
+          vec16 q = unpack_codes(bits, now.w[b][slice / 4][slice % 4 / 2 + 2 * (slice % 2)]);
+          if constexpr (DT == 0) q = centred(bits, q, -Q::BASE - (float)now.zero[b][g]);
 #pragma unroll
           for (int t = 0; t < NT; ++t) {
             if (sl == 0)
 #pragma unroll
               for (int i = 0; i < 16; ++i) v[b][t][i] = 0.f;
-            v[b][t] = mfma32<DT>(xs[t], q, v[b][t]);
+#pragma unroll
+            for (int p = 0; p < C::PARTS; ++p) v[b][t] = mfma32<DT>(xs[t][p], q, v[b][t]);
           }
         }
       }
       vec16 xsum[NT];
+      if (DT != 0) {
 #pragma unroll
-      for (int t = 0; t < NT; ++t) xsum[t] = *reinterpret_cast<const vec16*>(from + 32 * t * C::PITCH + 256 + g * 16);
+        for (int t = 0; t < NT; ++t) xsum[t] = *reinterpret_cast<const vec16*>(from + 32 * t * C::PITCH + 256 + g * 16);
+      }
 #pragma unroll
       for (int b = 0; b < kB; ++b) {
-        const uint32_t o = __builtin_bit_cast(uint16_t, T::narrow(-Q::BASE - (float)now.zero[b][g]));
-        const vec16 off = {half ? 0u : o | o << 16, half ? 0u : o, 0, 0};
         const float scale = T::widen(now.scale[b][g]);
+        if constexpr (DT != 0) {
+          const uint32_t o = __builtin_bit_cast(uint16_t, T::narrow(-Q::BASE - (float)now.zero[b][g]));
+          const vec16 off = {half ? 0u : o | o << 16, half ? 0u : o, 0, 0};
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          v[b][t] = mfma32<DT>(xsum[t], off, v[b][t]);
+          for (int t = 0; t < NT; ++t) v[b][t] = mfma32<DT>(xsum[t], off, v[b][t]);
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
           for (int i = 0; i < 16; ++i) sum[b][t][i] = __builtin_fmaf(scale, v[b][t][i], sum[b][t][i]);
-        }
       }
       if (!WHOLE) __builtin_amdgcn_sched_barrier(0);  // one group's sums at a time: registers
     }
@@ -323,21 +349,27 @@ __global__ __launch_bounds__(kThreads, 2) void q4_tile_kernel(const Q4Args a) {
 
 typedef void (*tile_fn)(const Q4Args);
 
-template <int DT, bool WORDS>
-tile_fn pick(int x_tiles, bool whole, bool zeros) {
-  if (!whole) return zeros ? q4_tile_kernel<DT, 2, false, true, WORDS> : q4_tile_kernel<DT, 2, false, false, WORDS>;
-  if (x_tiles == 1) return zeros ? q4_tile_kernel<DT, 1, true, true, WORDS> : q4_tile_kernel<DT, 1, true, false, WORDS>;
-  return zeros ? q4_tile_kernel<DT, 2, true, true, WORDS> : q4_tile_kernel<DT, 2, true, false, WORDS>;
+template <int DT, int NT, bool WHOLE>
+tile_fn pick(bool zeros, bool words) {
+  if (words) return zeros ? q4_tile_kernel<DT, NT, WHOLE, true, true> : q4_tile_kernel<DT, NT, WHOLE, false, true>;
+  return zeros ? q4_tile_kernel<DT, NT, WHOLE, true, false> : q4_tile_kernel<DT, NT, WHOLE, false, false>;
+}
+
+template <int DT>
+tile_fn pick(int x_tiles, bool whole, bool zeros, bool words) {
+  if (!whole) return pick<DT, 2, false>(zeros, words);
+  return x_tiles == 1 ? pick<DT, 1, true>(zeros, words) : pick<DT, 2, true>(zeros, words);
 }
 
 }  // namespace
 
 void launch_q4_tile(const Q4Args& a, int dtype, int x_tiles, unsigned grid, hipStream_t stream) {
-  const bool whole = a.group % 128 == 0;
+  const bool whole = a.group % 128 == 0, zeros = a.zeros != nullptr;
   const bool words = a.row_bytes % 4 == 0 && reinterpret_cast<uintptr_t>(a.codes) % 4 == 0;
-  const tile_fn fn = dtype == EBAG_F16 ? words ? pick<1, true>(x_tiles, whole, a.zeros) : pick<1, false>(x_tiles, whole, a.zeros)
-                     : words           ? pick<2, true>(x_tiles, whole, a.zeros)
-                                       : pick<2, false>(x_tiles, whole, a.zeros);
+  const tile_fn fn = dtype == EBAG_F16    ? pick<1>(x_tiles, whole, zeros, words)
+                     : dtype == EBAG_BF16 ? pick<2>(x_tiles, whole, zeros, words)
+                     : whole              ? pick<0, 1, true>(zeros, words)
+                                          : pick<0, 1, false>(zeros, words);
   hipLaunchKernelGGL(fn, dim3(grid), dim3(kThreads), 0, stream, a);
 }
 

@@ -155,7 +155,7 @@ def test_long_rows_and_many_weight_rows():
     _forward(rng, 2, 20011, 160, 32, "float16", True, 0, True, y_dtype="float32")
 
 
-@pytest.mark.parametrize("dtype", TYPES[1:])
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("rows,M,K,group,zeros,glu", [
     (400, 4100, 300, 128, True, 0), (389, 4610, 127, 128, False, 0), (400, 4100, 641, 256, False, 1),
     (1000, 4100, 700, 256, True, 0), (1027, 4098, 256, 128, True, 1), (1000, 8200, 333, 32, True, 0), (1010, 8202, 224, 96, False, 1)])
@@ -165,7 +165,7 @@ def test_forward_of_many_rows(rows, M, K, group, zeros, glu, dtype):
              step=5 if K % 2 else 0, shift=K % 2)
 
 
-@pytest.mark.parametrize("dtype", TYPES[1:])
+@pytest.mark.parametrize("dtype", TYPES)
 def test_forward_of_many_rows_exact(dtype):
     rng = np.random.default_rng(61)
     _forward(rng, 420, 4099, 260, 128, dtype, True, 0, True, y_dtype="float32", step=3, shift=1)
@@ -215,7 +215,7 @@ def test_experts(E, N, k, M, K, group, zeros, glu, dropped, gather, dtype):
     plan.close()
 
 
-@pytest.mark.parametrize("dtype", TYPES[1:])
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("gather", [False, True])
 @pytest.mark.parametrize("E,N,k,M,K,group,zeros,glu,dropped", [
     (40, 300, 2, 4098, 200, 128, True, 1, 40), (9, 700, 2, 4100, 260, 128, False, 0, 0), (9, 1400, 2, 4098, 161, 32, True, 1, 77),
