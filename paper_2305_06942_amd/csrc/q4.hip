@@ -195,11 +195,13 @@ int launch_few(const gemv_ar_q4_plan* h, Q4Args a, hipStream_t stream) {
   while (a.split < waves && a.split * 2 <= units && fits(a.split * 2) &&
          (all_tiles * a.split < 2048 || (rows < 4 && a.row_bytes > 1024 * a.split)))
     a.split *= 2;
-  // Its turns: about 2048 workgroups, or 1024 of twice the weights (128 experts of 2 x 1024 x 2048, two rows each: 66
-  // us with 2048, 63.5 with 1024, 60 with 512; 64 experts of 4096 x 2048, four rows each: 59, 66 and 102 us).
+  // Its turns: as many workgroups as the card's registers hold at a time, `held` to a CU, so that x is staged once and no
+  // place runs empty early (gated, 512 of them: 128 experts of 2 x 1024 x 2048, two rows each, with 512 workgroups 52.1
+  // us, 768 55.9, 1024 56.0, 384 61; one fp16 row x 65536 x 8192, 1024 of them: with 1024 56.7, 2048 60.0, 768 65.7).
   const int64_t turn_rows = 16 * (waves / a.split);
   const int64_t all_turns = (a.out_rows + turn_rows - 1) / turn_rows;
-  int64_t turns = all_turns * slots / (rt == 2 ? 1024 : 2048);
+  const int64_t held = (rt == 2 ? 8 : parts == 3 ? 12 : 16) / waves;
+  int64_t turns = all_turns * slots / (kCus * held);
   turns = turns < 1 ? 1 : turns > all_turns ? all_turns : turns;
   a.turns = (int)turns;
   const int64_t tiles = (all_turns + turns - 1) / turns;
@@ -212,7 +214,7 @@ int launch_few(const gemv_ar_q4_plan* h, Q4Args a, hipStream_t stream) {
   a.all_columns = units * columns;
   const int64_t all_x = (int64_t)rows * parts * (2 * (int64_t)a.all_columns + 16);
   const int64_t least = (int64_t)rows * parts * (2 * a.split * columns + 16);
-  const int64_t held = (rt == 2 ? 8 : parts == 3 ? 12 : 16) / waves, each = (tiles * slots + kCus - 1) / kCus, on_cu = each < held ? each : held;
+  const int64_t each = (tiles * slots + kCus - 1) / kCus, on_cu = each < held ? each : held;
   int64_t room = kCuLds / on_cu - (a.split > 1 ? sums : 0) - 16;
   if (room < all_x && all_x <= 40960) room = all_x;
   if (room < least) room = least;
