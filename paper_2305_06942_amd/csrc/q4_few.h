@@ -30,12 +30,11 @@ namespace {
 //
 // Bound by the codes' bytes with one to four rows: 65536 x 8192 fp16, one row, 277 MB
 // in 56 us, 4.9 TB/s (this pattern of 16 rows a wave reads 5.3 to 5.5 and a plain
-// stream 6.5; two thirds of the rest are the scales' loads); 128 experts of 2 x 1024 x
-// 2048, two rows each, 246 MB in 61 us.  A launch of a few MB is bound by its chain of
-// launch, x, codes, join and store: 4096 x 4096, one row, 5.5 us.  Many rows of x, or
-// scales for every 32 columns, bound it by the instructions of a block of 32 columns
-// (22 of the vector unit, 2 of the matrix unit) and by staging x: 12 x 10001 x 5001
-// 26 us, 60 experts of 1400 x 1000 with 20 rows each 28 us.
+// stream 6.5); 128 experts of 2 x 1024 x 2048, two rows each, 246 MB in 57 us.  A launch
+// of a few MB is bound by its chain of launch, x, codes, join and store: 4096 x 4096,
+// one row, 5.5 us.  Many rows of x, or scales for every 32 columns, bound it by the
+// latency of a unit's small steps and by staging x: 12 x 10001 x 5001 26 us, 60 experts
+// of 1400 x 1000 with 20 rows each 30 us, 22 with groups of 128.
 
 // Between lanes l, l + 16, l + 32, l + 48: w[t] of lane quarter c becomes w[c] of quarter t.
 __device__ __forceinline__ void transpose_words(vec16& w) {
