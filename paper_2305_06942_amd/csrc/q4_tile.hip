@@ -39,16 +39,16 @@ __device__ __forceinline__ float sum8(const vec16& v) {
   return ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
 }
 
-// A float as the first three elements of a vector, exactly: three bf16 (8 bits
-// each), or three fp16 (11 bits each).
-template <int DT>
+// A float as the first three elements of a vector, exactly: three bf16 of 8 bits each, with
+// fp16 x too, whose range ends at 65504 where a sum of its elements goes on.
 __device__ __forceinline__ vec16 three_parts(float f) {
+  typedef Type<2> T;
   uint32_t p[3];
 #pragma unroll
   for (int i = 0; i < 3; ++i) {
-    const typename Type<DT>::elt e = Type<DT>::narrow(f);
+    const T::elt e = T::narrow(f);
     p[i] = __builtin_bit_cast(uint16_t, e);
-    f -= Type<DT>::widen(e);
+    f -= T::widen(e);
   }
   return vec16{p[0] | p[1] << 16, p[2], 0, 0};
 }
@@ -72,7 +72,7 @@ struct Tile {
 // numbers BASE + q in registers and are multiplied from there, so every weight is
 // unpacked once for BN rows.  A group's sums start at zero, are corrected for BASE
 // and the zero point, and are added to the tile's sums times the scale.  The
-// correction, -(BASE + zero) * (sum of x), is one more matrix instruction: the
+// correction, -(BASE + zero) * (sum of x), is one more matrix instruction, in bf16: the
 // sum of x is found when x is staged and lies behind its row in three parts, whose
 // sum is exact, and the other operand is -(BASE + zero) three times.  With fp32 x BASE
 // and zero come off the codes, and three parts of x are multiplied with them (2048 x
@@ -220,7 +220,7 @@ __global__ __launch_bounds__(kThreads, 2) void q4_tile_kernel(const Q4Args a) {
         *reinterpret_cast<vec16*>(row + 16 * i * C::PITCH + chunk * 16) = pair_order(v[i][0]);
       }
       if ((WHOLE ? chunk : chunk & 3) < C::STAGED)
-        *reinterpret_cast<vec16*>(row + 16 * pick * C::PITCH + 256 + (WHOLE ? 0 : chunk / 4 * 16)) = three_parts<DT>(mine);
+        *reinterpret_cast<vec16*>(row + 16 * pick * C::PITCH + 256 + (WHOLE ? 0 : chunk / 4 * 16)) = three_parts(mine);
     }
   };
 
@@ -304,10 +304,10 @@ __global__ __launch_bounds__(kThreads, 2) void q4_tile_kernel(const Q4Args a) {
       for (int b = 0; b < kB; ++b) {
         const float scale = T::widen(now.scale[b][g]);
         if constexpr (DT != 0) {
-          const uint32_t o = __builtin_bit_cast(uint16_t, T::narrow(-Q::BASE - (float)now.zero[b][g]));
+          const uint32_t o = __builtin_bit_cast(uint16_t, Type<2>::narrow(-Q::BASE - (float)now.zero[b][g]));  // 143 at most: 8 bits
           const vec16 off = {half ? 0u : o | o << 16, half ? 0u : o, 0, 0};
 #pragma unroll
-          for (int t = 0; t < NT; ++t) v[b][t] = mfma32<DT>(xsum[t], off, v[b][t]);
+          for (int t = 0; t < NT; ++t) v[b][t] = mfma32<2>(xsum[t], off, v[b][t]);
         }
 #pragma unroll
         for (int t = 0; t < NT; ++t)
