@@ -414,14 +414,26 @@ __global__ __launch_bounds__(kRowThreads) void moe_combine_backward_kernel(const
         for (int u = 0; u < U; ++u) {
           float g[T::N], s[T::N];
           T::widen(y[i][u], g);
-          if (a.twice && v + u * at.lanes == a.vecs - 1) {
-#pragma unroll
-            for (int n = 0; n < T::N; ++n) g[n] = n < a.twice ? 0.f : g[n];
-          }
+          // Elements that the last vector repeats count once, whatever they hold: 0 in place of one factor alone would
+          // make an infinity in the other a NaN.
+          const bool repeats = a.twice && v + u * at.lanes == a.vecs - 1;
 #pragma unroll
           for (int n = 0; n < T::N; ++n) {
-            s[n] = p < kept ? w * f[u][n] : 0.f;
-            if (p < kept) dot[i] = __builtin_fmaf(f[u][n], g[n], dot[i]);
+            // Rounded to fp32 and then to the type, in every instance: the empty statement keeps the compiler from an
+            // instruction that rounds a product to fp16 at once.
+            s[n] = w * f[u][n];
+            asm("" : "+v"(s[n]));
+            s[n] = p < kept ? s[n] : 0.f;
+          }
+          if (p < kept) {
+            if (repeats) {
+#pragma unroll
+              for (int n = 0; n < T::N; ++n)
+                if (n >= a.twice) dot[i] = __builtin_fmaf(f[u][n], g[n], dot[i]);
+            } else {
+#pragma unroll
+              for (int n = 0; n < T::N; ++n) dot[i] = __builtin_fmaf(f[u][n], g[n], dot[i]);
+            }
           }
           if (v + u * at.lanes < a.vecs) store_row<STREAM == BOTH>(a.out + p * a.ld_out + byte_of(a, v + u * at.lanes), T::narrow(s));
         }
