@@ -551,10 +551,10 @@ int row_args(ebag_a2a_moe_plan* h, int64_t dim, int32_t dtype, int64_t tokens, c
   a->S = (uint32_t)(tokens * h->choices);
   a->choices = h->choices;
   a->experts = h->experts;
-  const int32_t bytes = (int32_t)(dim * elt);
-  a->vecs = bytes < 16 ? 0 : (bytes + 15) / 16;
-  a->last = bytes - 16;
-  a->twice = bytes < 16 ? 0 : (a->vecs * 16 - bytes) / elt;
+  const int64_t bytes = dim * elt;  // up to 2^31 - 4
+  a->vecs = bytes < 16 ? 0 : (int32_t)((bytes + 15) / 16);
+  a->last = (int32_t)(bytes - 16);
+  a->twice = bytes < 16 ? 0 : (int32_t)((a->vecs * 16LL - bytes) / elt);
   a->tail = bytes < 16 ? (int32_t)dim : 0;
   a->lanes = 1;
   while (a->lanes < 64 && a->lanes < a->vecs) a->lanes *= 2;

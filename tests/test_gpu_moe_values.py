@@ -50,3 +50,36 @@ def test_an_infinity_in_any_column_of_dout_is_an_infinite_gradient(D, dtype):
         assert torch.equal(dw[n], rows[n, :, c] * float("inf")), (n, c, dw[n])
     assert torch.equal(dw[N - 1], rows[N - 1].sum(1))
     plan.close()
+
+
+@pytest.mark.parametrize("D", [(1 << 29) - 1, (1 << 29) - 3, (1 << 29) - 4])
+def test_the_widest_rows(D):
+    """fp32 rows of just under 2^31 bytes, the most there may be: every column
+    is moved, the last ones too.  ys are +-1 and -+1 in turn and dout 1 in eight
+    columns only, so the dot product is a whole number."""
+    import torch
+    plan, offsets, pos = _plan_of(1, 1, 1, 0)
+    x = torch.zeros((1, D), device="cuda")
+    at = torch.tensor([0, 1, 2, D // 2, D - 4, D - 3, D - 2, D - 1], device="cuda")
+    values = torch.arange(1.0, 9.0, device="cuda")
+    x[0, at] = values
+    y = torch.full_like(x, float("nan"))
+    plan.dispatch(x, offsets, pos, y)
+    assert torch.equal(x, y)
+    w = torch.full((1, 1), 2.0, device="cuda")
+    y.fill_(float("nan"))
+    plan.combine(x, offsets, pos, w, y)
+    assert torch.equal(y, x * 2)
+    y.fill_(float("nan"))
+    plan.dispatch_backward(x, offsets, pos, y)
+    assert torch.equal(y, x)
+    ys = torch.ones_like(x)
+    ys[0, 1::2] = -1.0
+    y.fill_(float("nan"))
+    dw = torch.full_like(w, float("nan"))
+    plan.combine_backward(x, ys, offsets, pos, w, y, dw)
+    assert torch.equal(y, x * 2)
+    assert float(dw) == float((values * ys[0, at]).sum())
+    plan.close()
+    del x, y, ys
+    torch.cuda.empty_cache()
