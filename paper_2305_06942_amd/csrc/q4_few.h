@@ -220,8 +220,8 @@ __device__ __forceinline__ void stage_x(const Q4Args& a, uint32_t first, int row
       const uint32_t r = divide_by(by8, i), c = i - r * by8.d;
       int64_t row = a.src ? (int64_t)divide_by(a.by_choices, (uint32_t)a.src[first + r] & 0x7fffffffu) : (int64_t)(first + r);
       row = row < a.x_rows ? row : a.x_rows - 1;
-      const int k = k0 + 8 * (int)c;
-      load_x<DT>(a.x + row * a.ldx + (int64_t)k * ELT, a.K - k, a.K, v[j]);
+      const int on = 8 * (int)c;  // k0 + on may pass 2^31, K - k0 is positive
+      load_x<DT>(a.x + row * a.ldx + ((int64_t)k0 + on) * ELT, a.K - k0 - on, a.K, v[j]);
       to[j] = lds + r * pitch + c * 16;
     }
 #pragma unroll

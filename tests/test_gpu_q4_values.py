@@ -50,3 +50,31 @@ def test_large_values_of_one_sign(rows, M, group, zeros, dtype):
     x64 = 512.0 * rng.integers(1, 118, size=(rows, K))
     y = _forward(w, torch.from_numpy(x64).to(getattr(torch, dtype)).cuda(), M, K, group, dtype)
     assert np.array_equal(y.double().cpu().numpy(), x64 @ w.w64[0].T)
+
+
+@pytest.mark.parametrize("K,dtype", [((1 << 31) - 4097, "float16"), ((1 << 31) - 4099, "bfloat16")])
+def test_the_longest_rows(K, dtype):
+    """The most columns there may be: x is staged in parts, the last of which
+    ends behind 2^31.  A thousand columns of x are not zero, the last ones
+    among them; whole numbers below 2^24."""
+    import torch
+    import paper_2305_06942_amd as ebag
+    M, group = 2, 1 << 30
+    rng = np.random.default_rng(72)
+    codes = torch.randint(0, 256, (1, M, (K + 1) // 2), dtype=torch.uint8, device="cuda")
+    scales = torch.tensor([[[1.0, 2.0], [0.5, 1.0]]], dtype=getattr(torch, dtype), device="cuda")
+    at = np.unique(np.concatenate([rng.integers(0, K, size=980), np.arange(K - 10, K), [0, group - 1, group, 2 * group - 5000]]))
+    values = rng.integers(-9, 10, size=len(at)).astype(np.float64)
+    cols = torch.from_numpy(at).cuda()
+    x = torch.zeros((1, K), dtype=scales.dtype, device="cuda")
+    x[0, cols] = torch.from_numpy(values).to(x.dtype).cuda()
+    y = torch.full((1, M), float("nan"), device="cuda")
+    plan = ebag.Q4Gemv(M, K, group, _abi(dtype))
+    plan.forward(codes, scales, None, x, y)
+    byte = codes[0][:, cols // 2].cpu().numpy()
+    q = np.where(at % 2, byte >> 4, byte & 15) - 8.0
+    want = (q * scales[0].double().cpu().numpy()[:, at // group]) @ values
+    assert np.array_equal(y[0].double().cpu().numpy(), want)
+    plan.close()
+    del codes, x
+    torch.cuda.empty_cache()
