@@ -4,6 +4,7 @@
 #include "gemv_ar.h"
 #include "lanes.h"
 #include "q4.h"
+#include "q4_rows.h"
 
 namespace ebag {
 namespace {
@@ -169,9 +170,10 @@ __global__ __launch_bounds__(kThreads, 2) void q4_tile_kernel(const Q4Args a) {
       }
     if (!WORDS) {
 #pragma unroll
-      for (int b = 0; b < kB; ++b) {  // a row on a multiple of 4 needs no word behind
-        const uint8_t* p = codes[b] + (int64_t)step * (kStep / 2) + codes_at[b] + (64 - 16 * half - (shift[b] ? 0 : 4));
-        if (tail && p >= a.codes + a.codes_bytes) p = codes[b] + codes_at[b];  // not used: any word of the row
+      for (int b = 0; b < kB; ++b) {
+        const uint8_t* row = codes[b] + (int64_t)step * (kStep / 2) + (codes_at[b] - 16 * half);
+        const uint8_t* p = tail ? word_behind(row, kStep / 2, shift[b], a.codes + a.codes_bytes)
+                                : row + (kStep / 2 - (shift[b] ? 0 : 4));
         o.behind[b] = *reinterpret_cast<const uint32_t*>(p);
       }
     }

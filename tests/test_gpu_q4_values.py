@@ -78,3 +78,21 @@ def test_the_longest_rows(K, dtype):
     plan.close()
     del codes, x
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("group", [32, 128])
+@pytest.mark.parametrize("K", [1, 3, 6, 8, 13, 20, 27, 30, 31, 33])
+def test_many_rows_of_few_columns(K, group, dtype):
+    """Rows of codes of one to seventeen bytes in the matrix-product kernel, at
+    every distance from a multiple of 4, the last one at its allocation's end."""
+    import torch
+    rng = np.random.default_rng([73, K, group])
+    rows, M = 1000, 8199
+    x64 = rng.integers(-9, 10, size=(rows, K)).astype(np.float64)
+    x = torch.from_numpy(x64).to(getattr(torch, dtype)).cuda()
+    for at in range(4):
+        w = Weights(rng, 1, M, K, group, dtype, True, exact=True, at=at)
+        y = _forward(w, x, M, K, group, dtype)
+        want = torch.from_numpy(x64).cuda() @ torch.from_numpy(np.ascontiguousarray(w.w64[0].T)).cuda()
+        assert torch.equal(y.double(), want), at
