@@ -415,7 +415,9 @@ typedef struct ebag_a2a_moe_plan* ebag_a2a_moe_t;
  * must be made with the plan's device current (EBAG_EINVAL otherwise).  One
  * sort may be in flight per plan, checked as the forward's is (EBAG_EBUSY);
  * the other calls share nothing and may run on any stream.  All can be
- * captured into a graph and replayed. */
+ * captured into a graph and replayed; replays are not checked, so a graph with a
+ * sort of more than 4096 choices must be ordered with the plan's other sorts of
+ * that size, eager ones and other graphs'. */
 int ebag_a2a_moe_create(ebag_a2a_moe_t* out, int64_t max_tokens, int32_t choices, int32_t experts);
 
 /* Sort the choices: experts_of int32 [tokens][choices] -> offsets int32

@@ -519,12 +519,10 @@ int check_busy(gemv_ar_plan* h, hipStream_t stream) {
   return EBAG_OK;
 }
 
-// Remember the forward just enqueued on `stream` (not under graph capture).
+// Remember the forward just enqueued on `stream`.  A captured one runs nothing:
+// the last eager forward remains the one in flight.
 int note_forward(gemv_ar_plan* h, hipStream_t stream) {
-  if (capturing(stream)) {
-    h->fwd_pending = false;
-    return EBAG_OK;
-  }
+  if (capturing(stream)) return EBAG_OK;
   const hipError_t e = hipEventRecord(h->fwd_done, stream);
   if (e != hipSuccess) return hipf(e, "record the forward's completion");
   h->fwd_stream = stream;

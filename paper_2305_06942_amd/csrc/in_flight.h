@@ -38,12 +38,10 @@ inline int check_busy(InFlight& f, hipStream_t stream, const char* what) {
   return EBAG_OK;
 }
 
-// Remember the call just enqueued on `stream` (not under graph capture).
+// Remember the call just enqueued on `stream`.  A captured one runs nothing: the
+// last eager call remains the one in flight.
 inline int note_call(InFlight& f, hipStream_t stream) {
-  if (capturing(stream)) {
-    f.pending = false;
-    return EBAG_OK;
-  }
+  if (capturing(stream)) return EBAG_OK;
   const hipError_t e = hipEventRecord(f.done, stream);
   if (e != hipSuccess) return fail(EBAG_EHIP, "record the call's completion: %s", hipGetErrorString(e));
   f.stream = stream;
