@@ -157,10 +157,12 @@ void gemv_ar_destroy(gemv_ar_t h);
  *
  * x rows are K elements of dtype (EBAG_F32, EBAG_F16 or EBAG_BF16), row r at
  * element r * ldx; y rows are of dtype or fp32 (y_dtype), row r at element
- * r * ldy; neither needs an alignment beyond its elements'.  Sums are fp32,
- * fp32 x counts with all its 24 bits, and a result is rounded once.  143 |x|
- * summed over 512 columns must stay finite in fp32.  A row of x with an infinity or
- * NaN gives infinities or NaN in its own row of y only.  Outputs must not
+ * r * ldy; neither needs an alignment beyond its elements'.  Sums are fp32 and a
+ * result is rounded once.  An fp32 y is as near as a product in fp32 (each product of a
+ * weight's code less its zero point and x is exact; fp32 x counts with all its 24
+ * bits, down to 2^-133).  A 16-bit y has up to 4 of the 24 bits of its sums less: they hold
+ * up to 143 |x|, which summed over 512 columns must stay finite in fp32.  A row of x
+ * with an infinity or NaN gives infinities or NaN in its own row of y only.  Outputs must not
  * overlap inputs.  Results do not depend on the other rows' values and are the
  * same bits on every run.
  */

@@ -27,7 +27,6 @@ struct Q4Args {
   int32_t K, group, groups;
   int32_t experts;
   int32_t glu;
-  int32_t y_f32;
   Divisor by_choices;
   Divisor by_group_blocks;  // group / 32
   Divisor by_tiles;         // workgroups that share the rows of x, each with its rows of weights
@@ -42,6 +41,7 @@ struct Q4Args {
 };
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
@@ -50,10 +50,11 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 // of its mantissa, or above it) and exact; BASE and the zero point come off again
 // as (BASE + zero) * (the sum of x over the group).  The sums grow by BASE / 8 at
 // most that way, so fp32 loses 3 bits (fp16) or 4 (bf16) of its 24: fewer than the
-// results' rounding to 11 and 8 bits does, and the larger BASE leaves one code of
-// four where it is and saves its shift.  fp32 x goes as three bf16 parts whose sum
-// is x, bit for bit, so its products are exact too; its results keep all their bits,
-// so there BASE + zero comes off each code before the products (`centred`).
+// rounding of y to 11 and 8 bits does, and the larger BASE leaves one code of
+// four where it is and saves its shift.  An fp32 y keeps all its bits, so there BASE +
+// zero comes off each code before the products (`centred`; Y32 in the kernels).  fp32 x
+// goes as three bf16 parts whose sum is x, bit for bit (but for bits below 2^-133), so
+// its products are exact too.
 template <int DT> struct Q4Type;
 
 template <> struct Q4Type<1> {
@@ -84,15 +85,16 @@ template <> struct Q4Type<0> : Q4Type<2> {
 };
 
 // MASK and HIGH in registers: as literals they would take an instruction each,
-// and from one scalar and one vector register both go into one.  fp32: 1 in the
-// lower and in the upper half, too (as an inline constant 1.0 stands in the upper one).
-template <int DT>
+// and from one scalar and one vector register both go into one.  For `centred` bf16
+// codes 1 in the lower and in the upper half, too (as an inline constant 1.0 stands in
+// the upper one).
+template <int DT, bool Y32>
 struct CodeBits {
   uint32_t mask, high, lower, upper;
   __device__ __forceinline__ CodeBits() {
     asm volatile("s_mov_b32 %0, %1" : "=s"(mask) : "i"(Q4Type<DT>::MASK));
     asm volatile("v_mov_b32 %0, %1" : "=v"(high) : "i"(Q4Type<DT>::HIGH));
-    if (DT == 0) {
+    if (Y32 && DT != 1) {
       asm volatile("s_mov_b32 %0, 0x3f80" : "=s"(lower));
       asm volatile("s_mov_b32 %0, 0x3f800000" : "=s"(upper));
     }
@@ -100,18 +102,29 @@ struct CodeBits {
 };
 
 // Eight codes of a word as BASE + q, in the order 0 4, 1 5, 2 6, 3 7.
-template <int DT>
-__device__ __forceinline__ vec16 unpack_codes(const CodeBits<DT>& c, uint32_t w) {
+template <int DT, bool Y32>
+__device__ __forceinline__ vec16 unpack_codes(const CodeBits<DT, Y32>& c, uint32_t w) {
   vec16 r;
 #pragma unroll
   for (int j = 0; j < 4; ++j) r[j] = (Q4Type<DT>::pair(w, j) & c.mask) | c.high;
   return r;
 }
 
-// Eight bf16 numbers BASE + q with off = -(BASE + zero) added: q - zero, exact.  A dot
-// product with (1, 0) or (0, 1) widens one of two and adds in one instruction.
-__device__ __forceinline__ vec16 centred(const CodeBits<0>& c, const vec16& codes, float off) {
+// Eight numbers BASE + q with off = -(BASE + zero) added: q - zero, exact.  fp16: two at
+// a time.  bf16: a dot product with (1, 0) or (0, 1) widens one of two and adds in one
+// instruction.
+template <int DT>
+__device__ __forceinline__ vec16 centred(const CodeBits<DT, true>& c, const vec16& codes, float off) {
   vec16 r;
+  if (DT == 1) {
+    const f16x2 both = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_pkrtz(off, off));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t two = codes[j];
+      r[j] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, two) + both);
+    }
+    return r;
+  }
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const uint32_t two = codes[j];
@@ -256,17 +269,25 @@ __device__ __forceinline__ bool find_tile(const Q4Args& a, uint32_t slot, uint32
   return false;
 }
 
-template <int DT>
+template <int DT, bool Y32>
 __device__ __forceinline__ void store_y(const Q4Args& a, uint32_t n, int64_t m, float v) {
   typedef Type<DT> T;
   char* p = a.y + n * a.ldy;
-  if (DT == 0 || a.y_f32)
+  if (Y32)
     reinterpret_cast<float*>(p)[m] = v;
   else
     reinterpret_cast<typename T::elt*>(p)[m] = T::narrow(v);
 }
 
-__device__ __forceinline__ float silu(float v) { return v / (1.f + __expf(-v)); }
+// v / (1 + exp(-v)).  With the short exponential, off by (|v| + 8) 2^-22, where y is rounded
+// to 16 bits; an fp32 y gets the full one, of -|v|, which does not overflow where the
+// result is still a number.
+template <bool Y32>
+__device__ __forceinline__ float silu(float v) {
+  if (!Y32) return v / (1.f + __expf(-v));
+  const float e = expf(-fabsf(v));
+  return v * ((v < 0.f ? e : 1.f) / (1.f + e));
+}
 
 typedef void (*q4_fn)(const Q4Args);
 
@@ -276,6 +297,7 @@ struct Q4FewKind {
   bool whole;   // a group is a multiple of 128 columns
   bool zeros;   // there are zero points
   bool words;   // rows of codes begin at multiples of 4 bytes
+  bool y32;     // y is fp32
 };
 q4_fn pick_q4_few_f32(const Q4FewKind& k);
 q4_fn pick_q4_few_f16(const Q4FewKind& k);
@@ -285,6 +307,6 @@ q4_fn pick_q4_few_bf16(const Q4FewKind& k);
 // kQ4TileRows rows of weights (half as many outputs with glu) and 32 x_tiles (1 or
 // 2; fp32: 1) rows of x.
 constexpr int kQ4TileRows = 256;
-void launch_q4_tile(const Q4Args& a, int dtype, int x_tiles, unsigned grid, hipStream_t stream);
+void launch_q4_tile(const Q4Args& a, int dtype, bool y32, int x_tiles, unsigned grid, hipStream_t stream);
 
 }  // namespace ebag

@@ -160,7 +160,6 @@ int fill_args(const gemv_ar_q4_plan* h, const uint8_t* codes, const void* scales
   a->groups = (int32_t)((h->K + h->group - 1) / h->group);
   a->experts = h->experts;
   a->glu = h->glu;
-  a->y_f32 = y_dtype == EBAG_F32;
   a->by_choices = make_divisor(1);
   a->by_group_blocks = make_divisor(h->group / 32);
   return EBAG_OK;
@@ -173,7 +172,7 @@ int64_t most_tiles(int64_t rows, int64_t experts, int64_t cols) {
   return n < rows ? n : rows;
 }
 
-int launch_few(const gemv_ar_q4_plan* h, Q4Args a, hipStream_t stream) {
+int launch_few(const gemv_ar_q4_plan* h, Q4Args a, bool y32, hipStream_t stream) {
   const int rt = h->glu ? 2 : 1, parts = h->dtype == EBAG_F32 ? 3 : 1;
   const bool whole = h->group % 128 == 0;
   const int columns = whole ? 512 : 256;
@@ -227,20 +226,20 @@ int launch_few(const gemv_ar_q4_plan* h, Q4Args a, hipStream_t stream) {
   const int64_t some = a.fit_rows < rows ? rows * parts * (2 * (int64_t)a.some_columns + 16) : 0;
   a.x_bytes = (int)(all > some ? all : some);
   const size_t lds = a.x_bytes + (a.split > 1 ? sums : 0);
-  const Q4FewKind kind = {rt, whole, a.zeros != nullptr, a.row_bytes % 4 == 0 && reinterpret_cast<uintptr_t>(a.codes) % 4 == 0};
+  const Q4FewKind kind = {rt, whole, a.zeros != nullptr, a.row_bytes % 4 == 0 && reinterpret_cast<uintptr_t>(a.codes) % 4 == 0, y32};
   const q4_fn fn = h->dtype == EBAG_F32 ? pick_q4_few_f32(kind) : h->dtype == EBAG_F16 ? pick_q4_few_f16(kind) : pick_q4_few_bf16(kind);
   hipLaunchKernelGGL(fn, dim3((unsigned)(tiles * slots)), dim3(64 * waves), lds, stream, a);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? EBAG_OK : hipf(e, "launch the product with 4-bit weights");
 }
 
-int launch_tile(const gemv_ar_q4_plan* h, Q4Args a, int x_tiles, hipStream_t stream) {
+int launch_tile(const gemv_ar_q4_plan* h, Q4Args a, bool y32, int x_tiles, hipStream_t stream) {
   const int64_t cols = 32 * x_tiles, per_wg = kQ4TileRows / (h->glu ? 2 : 1);
   const int64_t tiles = (a.out_rows + per_wg - 1) / per_wg;
   const int64_t slots = a.offsets ? most_tiles(a.rows, h->experts, cols) : (a.rows + cols - 1) / cols;
   if (tiles * slots > INT_MAX) return fail(EBAG_EUNSUPPORTED, "too many tiles for one launch");
   a.by_tiles = make_divisor(tiles);
-  launch_q4_tile(a, h->dtype, x_tiles, (unsigned)(tiles * slots), stream);
+  launch_q4_tile(a, h->dtype, y32, x_tiles, (unsigned)(tiles * slots), stream);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? EBAG_OK : hipf(e, "launch the product with 4-bit weights");
 }
@@ -255,8 +254,9 @@ int launch_tile(const gemv_ar_q4_plan* h, Q4Args a, int x_tiles, hipStream_t str
 // 67.)  fp32 x: 16.5 ns; with 32 rows 235 ns and 64 us, or 272 ns and 85 us (one of 4096 x
 // 4096, in us by the two: 64 rows 34, 63; 512 rows 128, 69; 2048 rows 490, 234; with groups
 // of 32 523, 279).  An expert's rows fill their last tile half on average.
-int launch(const gemv_ar_q4_plan* h, const Q4Args& a, hipStream_t stream) {
-  if (h->K >= 1 << 27) return launch_few(h, a, stream);
+int launch(const gemv_ar_q4_plan* h, const Q4Args& a, int y_dtype, hipStream_t stream) {
+  const bool y32 = y_dtype == EBAG_F32;
+  if (h->K >= 1 << 27) return launch_few(h, a, y32, stream);
   const bool whole = h->group % 128 == 0;
   auto tiles = [&](double rows, double cols) {  // of `rows` weight rows and `cols` rows of x
     const double experts = a.offsets ? h->experts : 1, some = a.rows < experts ? a.rows : experts;
@@ -267,13 +267,13 @@ int launch(const gemv_ar_q4_plan* h, const Q4Args& a, hipStream_t stream) {
   auto at_least = [](double v, double least) { return v < least ? least : v; };
   if (h->dtype == EBAG_F32) {
     const double tile = at_least(tiles(kQ4TileRows, 32) * (whole ? 0.235 : 0.272), whole ? 64 : 85);
-    return tiles(16, 16) * 0.0165 <= tile ? launch_few(h, a, stream) : launch_tile(h, a, 1, stream);
+    return tiles(16, 16) * 0.0165 <= tile ? launch_few(h, a, y32, stream) : launch_tile(h, a, y32, 1, stream);
   }
   const double few = tiles(16, 16) * (whole ? 0.0080 : 0.0125);
   const double one = at_least(tiles(kQ4TileRows, 32) * 0.157, 45);
   const double two = at_least(tiles(kQ4TileRows, 64) * (whole ? 0.203 : 0.48), whole ? 62 : 107);
-  if (few <= two && (few <= one || !whole)) return launch_few(h, a, stream);
-  return launch_tile(h, a, whole && one <= two ? 1 : 2, stream);
+  if (few <= two && (few <= one || !whole)) return launch_few(h, a, y32, stream);
+  return launch_tile(h, a, y32, whole && one <= two ? 1 : 2, stream);
 }
 
 }  // namespace
@@ -347,7 +347,7 @@ int gemv_ar_q4_forward(gemv_ar_q4_t h, const uint8_t* codes, const void* scales,
   if (!rows) return EBAG_OK;
   Q4Args a;
   if (int rc = fill_args(h, codes, scales, zeros, x, ldx, rows, rows, y, ldy, y_dtype, &a)) return rc;
-  return launch(h, a, stream);
+  return launch(h, a, y_dtype, stream);
 }
 
 int gemv_ar_q4_experts(gemv_ar_q4_t h, const uint8_t* codes, const void* scales, const uint8_t* zeros, const void* x,
@@ -365,7 +365,7 @@ int gemv_ar_q4_experts(gemv_ar_q4_t h, const uint8_t* codes, const void* scales,
   a.offsets = offsets;
   a.src = src;
   a.by_choices = make_divisor(src ? choices : 1);
-  return launch(h, a, stream);
+  return launch(h, a, y_dtype, stream);
 }
 
 void gemv_ar_q4_destroy(gemv_ar_q4_t h) { delete h; }

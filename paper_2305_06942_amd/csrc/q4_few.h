@@ -60,14 +60,14 @@ __device__ __forceinline__ void gather_words(uint32_t w, uint32_t* all) {
 constexpr int kFewThreads = 512;
 
 // What a launch is compiled for.  WHOLE: a group is a multiple of 128 columns, so
-// a step of 128 has one scale.  ZEROS: there are zero points.  WORDS: rows of codes
+// a step of 128 has one scale.  ZEROS: there are zero points.  Y32: y is fp32.  WORDS: rows of codes
 // begin at multiples of 4 bytes.  Others are loaded from the multiple of 4 below and
 // shifted in registers: memory takes 16 bytes at any address, but not as fast (1 x
 // 40000 x 5110, rows of 2555 bytes: 43.9 us; rows of 2556: 28.7 us; shifted 32.7 us).
-template <int DT_, int RT_, bool WHOLE_, bool ZEROS_, bool WORDS_>
+template <int DT_, int RT_, bool WHOLE_, bool ZEROS_, bool WORDS_, bool Y32_>
 struct FewShape {
   static constexpr int DT = DT_, RT = RT_;
-  static constexpr bool WHOLE = WHOLE_, ZEROS = ZEROS_, WORDS = WORDS_;
+  static constexpr bool WHOLE = WHOLE_, ZEROS = ZEROS_, WORDS = WORDS_, Y32 = Y32_;
   static constexpr int STEPS = WHOLE ? 4 : 2;     // of a unit
   static constexpr int SCALES = WHOLE ? 1 : STEPS;  // loads of scales of a unit: four lanes of a row load one each
   static constexpr int COLUMNS = 128 * STEPS;
@@ -135,7 +135,7 @@ __device__ __forceinline__ void load_weights(const Q4Args& a, const Few<C>& f, U
 // unit's columns; the parts of fp32 x are `pitch` bytes apart.
 // shift: not WORDS: how many bytes a row begins behind a multiple of 4.
 template <class C>
-__device__ __forceinline__ void multiply(const CodeBits<C::DT>& bits, Unit<C>& o, const char* x, int pitch,
+__device__ __forceinline__ void multiply(const CodeBits<C::DT, C::Y32>& bits, Unit<C>& o, const char* x, int pitch,
                                          const uint32_t* shift, f32x4* sum) {
   typedef Q4Type<C::DT> Q;
   typedef Type<C::DT> T;
@@ -185,19 +185,19 @@ __device__ __forceinline__ void multiply(const CodeBits<C::DT>& bits, Unit<C>& o
       vec16 xs[PARTS];
 #pragma unroll
       for (int p = 0; p < PARTS; ++p) xs[p] = *reinterpret_cast<const vec16*>(x + p * pitch + (s * 4 + t) * 64);
-      if (!F32) xsum = Q::mfma(xs[0], ones, C::WHOLE && t ? xsum : f32x4{0, 0, 0, 0});
+      if (!C::Y32) xsum = Q::mfma(xs[0], ones, C::WHOLE && t ? xsum : f32x4{0, 0, 0, 0});
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
         const int g = C::WHOLE ? 0 : t;
         vec16 q = unpack_codes(bits, o.w[s][rt][t]);
-        if constexpr (F32) q = centred(bits, q, off[rt][g]);
+        if constexpr (C::Y32) q = centred(bits, q, off[rt][g]);
         if (!C::WHOLE || t == 0) v[rt] = f32x4{0, 0, 0, 0};
 #pragma unroll
         for (int p = 0; p < PARTS; ++p) v[rt] = Q::mfma(xs[p], q, v[rt]);
         if (C::WHOLE && t < 3) continue;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          sum[rt][i] = __builtin_fmaf(scale[rt][g], F32 ? v[rt][i] : __builtin_fmaf(off[rt][g], xsum[i], v[rt][i]), sum[rt][i]);
+          sum[rt][i] = __builtin_fmaf(scale[rt][g], C::Y32 ? v[rt][i] : __builtin_fmaf(off[rt][g], xsum[i], v[rt][i]), sum[rt][i]);
       }
     }
   }
@@ -257,7 +257,7 @@ __global__ __launch_bounds__(kFewThreads, C::RT == 2 ? 2 : C::DT == 0 ? 3 : 4) v
     for (uint32_t i = threadIdx.x; i < 16 * cols; i += blockDim.x) {
       const uint32_t n = first + i / cols;
       const int64_t m = wg_m0 + i % cols;
-      if (n < end && m < a.out_rows) store_y<DT>(a, n, m, 0.f);
+      if (n < end && m < a.out_rows) store_y<DT, C::Y32>(a, n, m, 0.f);
     }
     return;
   }
@@ -299,7 +299,7 @@ __global__ __launch_bounds__(kFewThreads, C::RT == 2 ? 2 : C::DT == 0 ? 3 : 4) v
   const int whole = a.K / C::COLUMNS, units = (a.K + C::COLUMNS - 1) / C::COLUMNS;
   const char* x = lds + (r16 < rows ? r16 : rows - 1) * pitch + quarter * 16;
   f32x4* sums = reinterpret_cast<f32x4*>(lds + a.x_bytes);
-  const CodeBits<DT> bits;
+  const CodeBits<DT, C::Y32> bits;
   f32x4 sum[RT];
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) sum[rt] = f32x4{0, 0, 0, 0};
@@ -331,7 +331,7 @@ __global__ __launch_bounds__(kFewThreads, C::RT == 2 ? 2 : C::DT == 0 ? 3 : 4) v
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const uint32_t n = first + 4 * quarter + k;
-          if (n < end) store_y<DT>(a, n, m, pair == 2 ? silu(sum[rt][k]) * sum[rt + 1 < RT ? rt + 1 : rt][k] : sum[rt][k]);
+          if (n < end) store_y<DT, C::Y32>(a, n, m, pair == 2 ? silu<C::Y32>(sum[rt][k]) * sum[rt + 1 < RT ? rt + 1 : rt][k] : sum[rt][k]);
         }
       }
     }
@@ -401,16 +401,22 @@ __global__ __launch_bounds__(kFewThreads, C::RT == 2 ? 2 : C::DT == 0 ? 3 : 4) v
 // The instance for a launch.
 template <int DT>
 q4_fn pick_few(const Q4FewKind& k) {
-  auto codes = [&](auto rt, auto whole) -> q4_fn {
+  auto codes = [&](auto rt, auto whole, auto y32) -> q4_fn {
     constexpr int RT = decltype(rt)::value;
-    constexpr bool WHOLE = decltype(whole)::value;
-    if (k.words) return k.zeros ? q4_few_kernel<FewShape<DT, RT, WHOLE, true, true>> : q4_few_kernel<FewShape<DT, RT, WHOLE, false, true>>;
-    return k.zeros ? q4_few_kernel<FewShape<DT, RT, WHOLE, true, false>> : q4_few_kernel<FewShape<DT, RT, WHOLE, false, false>>;
+    constexpr bool WHOLE = decltype(whole)::value, Y32 = decltype(y32)::value;
+    if (k.words)
+      return k.zeros ? q4_few_kernel<FewShape<DT, RT, WHOLE, true, true, Y32>> : q4_few_kernel<FewShape<DT, RT, WHOLE, false, true, Y32>>;
+    return k.zeros ? q4_few_kernel<FewShape<DT, RT, WHOLE, true, false, Y32>> : q4_few_kernel<FewShape<DT, RT, WHOLE, false, false, Y32>>;
+  };
+  auto result = [&](auto rt, auto whole) -> q4_fn {
+    if constexpr (DT != 0)
+      if (!k.y32) return codes(rt, whole, std::false_type());
+    return codes(rt, whole, std::true_type());
   };
   const std::integral_constant<int, 1> one;
   const std::integral_constant<int, 2> two;
-  if (k.tiles == 1) return k.whole ? codes(one, std::true_type()) : codes(one, std::false_type());
-  return k.whole ? codes(two, std::true_type()) : codes(two, std::false_type());
+  if (k.tiles == 1) return k.whole ? result(one, std::true_type()) : result(one, std::false_type());
+  return k.whole ? result(two, std::true_type()) : result(two, std::false_type());
 }
 
 }  // namespace

@@ -57,12 +57,12 @@ __device__ __forceinline__ vec16 three_parts(float f) {
 // WHOLE: a group is a multiple of 128 columns, so a step has one scale; otherwise
 // every block of 32 columns has its own (fp16 and bf16: only with 64 rows of x, as with
 // 32 the kernel for few rows is never slower; fp32: only 32, whose three parts fill LDS).
-template <int DT, int NT, bool WHOLE>
+template <int DT, int NT, bool WHOLE, bool Y32>
 struct Tile {
   static constexpr int BN = 32 * NT;                  // rows of x
   static constexpr int GROUPS = WHOLE ? 1 : 4;        // of a step
   static constexpr int PARTS = Q4Type<DT>::PARTS, VECS = DT == 0 ? 2 : 1, ELT = sizeof(typename Type<DT>::elt);
-  static constexpr int PITCH = DT == 0 || WHOLE ? 272 : 336;  // bytes of a row of x in LDS: 16 lanes' vectors on different banks
+  static constexpr int PITCH = Y32 || WHOLE ? 272 : 336;  // bytes of a row of x in LDS: 16 lanes' vectors on different banks
   static constexpr int PART = BN * PITCH;             // of one part of fp32 x
   static constexpr int STAGED = BN * 16 / kThreads;   // vectors of a thread
 };
@@ -75,8 +75,8 @@ struct Tile {
 // and the zero point, and are added to the tile's sums times the scale.  The
 // correction, -(BASE + zero) * (sum of x), is one more matrix instruction, in bf16: the
 // sum of x is found when x is staged and lies behind its row in three parts, whose
-// sum is exact, and the other operand is -(BASE + zero) three times.  With fp32 x BASE
-// and zero come off the codes, and three parts of x are multiplied with them (2048 x
+// sum is exact, and the other operand is -(BASE + zero) three times.  With fp32 y (Y32) BASE
+// and zero come off the codes; three parts of fp32 x are multiplied with them (2048 x
 // 4096 x 4096: 234 us, 294 TFLOP/s, 880 of the matrix unit's; fp32's own 154).
 //
 // Bound by the latency and the L1 work of its loads: 32768 rows on 64 experts of 4096 x
@@ -89,9 +89,9 @@ struct Tile {
 // WORDS: rows of codes begin at multiples of 4 bytes.  Others are loaded from the
 // multiple of 4 below and shifted in registers (32768 rows on 64 experts of 4096 x
 // 2044, rows of 1022 bytes: 1241 us loaded at their own addresses, 904 us shifted).
-template <int DT, int NT, bool WHOLE, bool ZEROS, bool WORDS>
+template <int DT, int NT, bool WHOLE, bool ZEROS, bool WORDS, bool Y32>
 __global__ __launch_bounds__(kThreads, 2) void q4_tile_kernel(const Q4Args a) {
-  typedef Tile<DT, NT, WHOLE> C;
+  typedef Tile<DT, NT, WHOLE, Y32> C;
   typedef Type<DT> T;
   typedef Q4Type<DT> Q;
   __shared__ __attribute__((aligned(16))) char lds[2][C::PARTS * C::PART];
@@ -109,7 +109,7 @@ __global__ __launch_bounds__(kThreads, 2) void q4_tile_kernel(const Q4Args a) {
     for (uint32_t i = tid; i < C::BN * cols; i += kThreads) {
       const uint32_t n = first + i / cols;
       const int64_t m = wg_m0 + i % cols;
-      if (n < end && m < a.out_rows) store_y<DT>(a, n, m, 0.f);
+      if (n < end && m < a.out_rows) store_y<DT, Y32>(a, n, m, 0.f);
     }
     return;
   }
@@ -211,6 +211,10 @@ __global__ __launch_bounds__(kThreads, 2) void q4_tile_kernel(const Q4Args a) {
         for (int p = 0; p < C::PARTS; ++p)
           *reinterpret_cast<vec16*>(row + p * C::PART + 16 * i * C::PITCH + chunk * 16) = parts[p];
       }
+    } else if constexpr (Y32) {
+#pragma unroll
+      for (int i = 0; i < C::STAGED; ++i)
+        *reinterpret_cast<vec16*>(row + 16 * i * C::PITCH + chunk * 16) = pair_order(v[i][0]);
     } else {
       // Lane `chunk` of a row (or of a quarter of it) finishes the sums of row number `chunk` % STAGED.
       float mine = 0.f;
@@ -226,7 +230,7 @@ __global__ __launch_bounds__(kThreads, 2) void q4_tile_kernel(const Q4Args a) {
     }
   };
 
-  const CodeBits<DT> bits;
+  const CodeBits<DT, Y32> bits;
   f32x16 sum[kB][NT];
 #pragma unroll
   for (int b = 0; b < kB; ++b)
@@ -286,7 +290,7 @@ __global__ __launch_bounds__(kThreads, 2) void q4_tile_kernel(const Q4Args a) {
         for (int b = 0; b < kB; ++b) {
           // Of each 64 columns, words 0 and 2 have the first 32, words 1 and 3 the others.
           vec16 q = unpack_codes(bits, now.w[b][slice / 4][slice % 4 / 2 + 2 * (slice % 2)]);
-          if constexpr (DT == 0) q = centred(bits, q, -Q::BASE - (float)now.zero[b][g]);
+          if constexpr (Y32) q = centred(bits, q, -Q::BASE - (float)now.zero[b][g]);
 #pragma unroll
           for (int t = 0; t < NT; ++t) {
             if (sl == 0)
@@ -298,14 +302,14 @@ __global__ __launch_bounds__(kThreads, 2) void q4_tile_kernel(const Q4Args a) {
         }
       }
       vec16 xsum[NT];
-      if (DT != 0) {
+      if (!Y32) {
 #pragma unroll
         for (int t = 0; t < NT; ++t) xsum[t] = *reinterpret_cast<const vec16*>(from + 32 * t * C::PITCH + 256 + g * 16);
       }
 #pragma unroll
       for (int b = 0; b < kB; ++b) {
         const float scale = T::widen(now.scale[b][g]);
-        if constexpr (DT != 0) {
+        if constexpr (!Y32) {
           const uint32_t o = __builtin_bit_cast(uint16_t, Type<2>::narrow(-Q::BASE - (float)now.zero[b][g]));  // 143 at most: 8 bits
           const vec16 off = {half ? 0u : o | o << 16, half ? 0u : o, 0, 0};
 #pragma unroll
@@ -344,34 +348,34 @@ __global__ __launch_bounds__(kThreads, 2) void q4_tile_kernel(const Q4Args a) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const uint32_t n = first + 32 * t + 8 * (i / 4) + 4 * half + i % 4;
-        if (n < end) store_y<DT>(a, n, m, pair == 2 ? silu(sum[0][t][i]) * sum[1][t][i] : sum[b][t][i]);
+        if (n < end) store_y<DT, Y32>(a, n, m, pair == 2 ? silu<Y32>(sum[0][t][i]) * sum[1][t][i] : sum[b][t][i]);
       }
   }
 }
 
 typedef void (*tile_fn)(const Q4Args);
 
-template <int DT, int NT, bool WHOLE>
+template <int DT, int NT, bool WHOLE, bool Y32>
 tile_fn pick(bool zeros, bool words) {
-  if (words) return zeros ? q4_tile_kernel<DT, NT, WHOLE, true, true> : q4_tile_kernel<DT, NT, WHOLE, false, true>;
-  return zeros ? q4_tile_kernel<DT, NT, WHOLE, true, false> : q4_tile_kernel<DT, NT, WHOLE, false, false>;
+  if (words) return zeros ? q4_tile_kernel<DT, NT, WHOLE, true, true, Y32> : q4_tile_kernel<DT, NT, WHOLE, false, true, Y32>;
+  return zeros ? q4_tile_kernel<DT, NT, WHOLE, true, false, Y32> : q4_tile_kernel<DT, NT, WHOLE, false, false, Y32>;
 }
 
-template <int DT>
+template <int DT, bool Y32>
 tile_fn pick(int x_tiles, bool whole, bool zeros, bool words) {
-  if (!whole) return pick<DT, 2, false>(zeros, words);
-  return x_tiles == 1 ? pick<DT, 1, true>(zeros, words) : pick<DT, 2, true>(zeros, words);
+  if (!whole) return pick<DT, 2, false, Y32>(zeros, words);
+  return x_tiles == 1 ? pick<DT, 1, true, Y32>(zeros, words) : pick<DT, 2, true, Y32>(zeros, words);
 }
 
 }  // namespace
 
-void launch_q4_tile(const Q4Args& a, int dtype, int x_tiles, unsigned grid, hipStream_t stream) {
+void launch_q4_tile(const Q4Args& a, int dtype, bool y32, int x_tiles, unsigned grid, hipStream_t stream) {
   const bool whole = a.group % 128 == 0, zeros = a.zeros != nullptr;
   const bool words = a.row_bytes % 4 == 0 && reinterpret_cast<uintptr_t>(a.codes) % 4 == 0;
-  const tile_fn fn = dtype == EBAG_F16    ? pick<1>(x_tiles, whole, zeros, words)
-                     : dtype == EBAG_BF16 ? pick<2>(x_tiles, whole, zeros, words)
-                     : whole              ? pick<0, 1, true>(zeros, words)
-                                          : pick<0, 1, false>(zeros, words);
+  const tile_fn fn = dtype == EBAG_F16    ? y32 ? pick<1, true>(x_tiles, whole, zeros, words) : pick<1, false>(x_tiles, whole, zeros, words)
+                     : dtype == EBAG_BF16 ? y32 ? pick<2, true>(x_tiles, whole, zeros, words) : pick<2, false>(x_tiles, whole, zeros, words)
+                     : whole              ? pick<0, 1, true, true>(zeros, words)
+                                          : pick<0, 1, false, true>(zeros, words);
   hipLaunchKernelGGL(fn, dim3(grid), dim3(kThreads), 0, stream, a);
 }
 

@@ -96,3 +96,52 @@ def test_many_rows_of_few_columns(K, group, dtype):
         y = _forward(w, x, M, K, group, dtype)
         want = torch.from_numpy(x64).cuda() @ torch.from_numpy(np.ascontiguousarray(w.w64[0].T)).cuda()
         assert torch.equal(y.double(), want), at
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,M,group", LAUNCHES)
+def test_fp32_results_are_as_near_as_an_fp32_product(rows, M, group, dtype):
+    """4096 columns of normal x: the root mean square distance from the result in
+    64 bits is at most twice that of the same product in fp32 by torch; and no
+    result is further off than the sum of |weight * x|, whose terms are exact,
+    times 2^-23 for each of at most 128 products of a group in a chain, a
+    multiply-add per 32 columns and 16 partial sums."""
+    import torch
+    rng = np.random.default_rng([74, rows, group])
+    K = 4096
+    w = Weights(rng, 1, M, K, group, dtype, True, at=0)
+    x = torch.from_numpy(rng.standard_normal((rows, K))).to(getattr(torch, dtype)).cuda()
+    y = _forward(w, x, M, K, group, dtype).double()
+    w64 = torch.from_numpy(np.ascontiguousarray(w.w64[0].T)).cuda()
+    want = x.double() @ w64
+    far = (y - want).abs()
+    assert bool((far <= (144 + K / 16) * 2.0 ** -23 * (x.double().abs() @ w64.abs())).all())
+    plain = x.float() @ w64.float()
+    rms = lambda v: float(v.square().mean().sqrt())  # noqa: E731
+    assert rms(far) <= 2 * rms(plain.double() - want), (rms(far), rms(plain.double() - want))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,M", [(3, 512), (1000, 8200)])
+def test_silu_in_fp32(rows, M, dtype):
+    """One column of x is 1, the gates are a scale times -8 .. 7, rounded to fp32 where
+    the scale has 24 bits, and the up weights 1, so y is silu of a known number.  An exponential good to one unit in the
+    last place (2^-23), 1 + e, a division and two products of 2^-24 each make
+    2^-21; an exponential below 2^-126 is off by 2^-149, times |gate| below 128."""
+    import torch
+    rng = np.random.default_rng([75, rows])
+    K = group = 32
+    w = Weights(rng, 1, M, K, group, dtype, False, at=0)
+    half = M // 2
+    scales = torch.empty((1, M, 1), dtype=torch.float64)
+    scales[0, :half, 0] = torch.from_numpy(np.concatenate([np.linspace(0.01, 13, half - 56), 12.99 - np.linspace(0, 2, 56)]))
+    scales[0, half:] = 1
+    w.scales = scales.to(getattr(torch, dtype)).cuda()
+    w.codes[0, half:] = 0x99
+    x = torch.zeros((rows, K), dtype=w.scales.dtype, device="cuda")
+    x[:, 0] = 1
+    y = _forward(w, x, M, K, group, dtype, glu=1).double().cpu().numpy()
+    g = (w.scales[0, :half, 0].double().cpu().numpy() * ((w.codes[0, :half, 0].cpu().numpy() & 15) - 8.0)).astype(np.float32).astype(np.float64)
+    want = g * np.where(g < 0, np.exp(-np.abs(g)), 1.0) / (1 + np.exp(-np.abs(g)))
+    assert g.min() < -90 and g.max() > 80
+    assert np.all(np.abs(y - want) <= 2.0 ** -21 * np.abs(want) + 128 * 2.0 ** -149)
