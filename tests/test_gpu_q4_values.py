@@ -145,3 +145,51 @@ def test_silu_in_fp32(rows, M, dtype):
     want = g * np.where(g < 0, np.exp(-np.abs(g)), 1.0) / (1 + np.exp(-np.abs(g)))
     assert g.min() < -90 and g.max() > 80
     assert np.all(np.abs(y - want) <= 2.0 ** -21 * np.abs(want) + 128 * 2.0 ** -149)
+
+
+@pytest.mark.parametrize("zeros", [False, True])
+@pytest.mark.parametrize("rows,M,group", LAUNCHES)
+def test_every_bit_of_fp32_x_counts(rows, M, group, zeros):
+    """One column of each row of x is not zero and has 24 bits; the weight there is
+    a power of two times a code less its zero point that is one, too: the
+    product is known bit for bit, whatever the other columns' weights are."""
+    import torch
+    rng = np.random.default_rng([76, rows, group])
+    K = 260
+    w = Weights(rng, 1, M, K, group, "float32", zeros, exact=True, at=0)
+    at = rng.integers(0, K, size=rows)
+    significand = rng.integers(1 << 23, 1 << 24, size=rows) | 1
+    v = np.where(rng.random(rows) < 0.5, -1.0, 1.0) * significand * 2.0 ** rng.integers(-60, 60, size=rows)
+    x = torch.zeros((rows, K), device="cuda")
+    x[torch.arange(rows), torch.from_numpy(at).cuda()] = torch.from_numpy(v.astype(np.float32)).cuda()
+    y = _forward(w, x, M, K, group, "float32").double().cpu().numpy()
+    weight = w.w64[0][:, at].T  # [rows, M]
+    m, _ = np.frexp(np.abs(weight))
+    known = (m == 0.5) | (weight == 0)
+    assert known.mean() > 0.2
+    assert np.array_equal(y[known], (weight * v[:, None])[known])
+    # Others: (q - zero) x of up to 28 bits is rounded to 24 once by each of three additions.
+    assert np.all(np.abs(y - weight * v[:, None]) <= 3 * 2.0 ** -23 * np.abs(weight * v[:, None]))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("y32", [False, True])
+@pytest.mark.parametrize("rows,M,group", LAUNCHES)
+def test_rows_are_their_own(rows, M, group, y32, dtype):
+    """Every row's result is the same bits whatever the other rows hold; a row
+    with an infinity or NaN has no finite result."""
+    import torch
+    rng = np.random.default_rng([77, rows, group])
+    K = 500
+    w = Weights(rng, 1, M, K, group, dtype, True, at=0)
+    x = torch.from_numpy(rng.standard_normal((rows, K))).to(getattr(torch, dtype)).cuda()
+    y_dtype = "float32" if y32 else dtype
+    clean = _forward(w, x, M, K, group, dtype, y_dtype)
+    bad = np.unique(np.concatenate([[0, rows - 1], rng.integers(0, rows, size=rows // 5)]))
+    value = torch.tensor([float("inf"), float("-inf"), float("nan")], dtype=x.dtype, device="cuda")
+    x[torch.from_numpy(bad).cuda(), torch.from_numpy(rng.integers(0, K, size=len(bad))).cuda()] = value[torch.arange(len(bad), device="cuda") % 3]
+    dirty = _forward(w, x, M, K, group, dtype, y_dtype)
+    good = torch.ones(rows, dtype=torch.bool, device="cuda")
+    good[torch.from_numpy(bad).cuda()] = False
+    assert torch.equal(clean[good], dirty[good])
+    assert not torch.isfinite(dirty[~good]).any()
