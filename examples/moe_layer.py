@@ -21,6 +21,7 @@ import os
 import sys
 
 import torch
+from torch.autograd.function import once_differentiable
 
 sys.path.insert(0, os.path.join(os.path.dirname(os.path.abspath(__file__)), ".."))
 
@@ -94,6 +95,7 @@ class _Dispatch(torch.autograd.Function):
         return xs
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dxs):
         offsets, pos = ctx.saved_tensors
         dx = torch.empty(ctx.shape, dtype=dxs.dtype, device=dxs.device)
@@ -111,6 +113,7 @@ class _Combine(torch.autograd.Function):
         return out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout):
         ys, weights, offsets, pos = ctx.saved_tensors
         dys, dweights = torch.empty_like(ys), torch.empty_like(weights)
