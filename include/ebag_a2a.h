@@ -410,7 +410,7 @@ void ebag_a2a_destroy(ebag_a2a_t h);
 typedef struct ebag_a2a_moe_plan* ebag_a2a_moe_t;
 
 /* Create a plan on the current HIP device for up to max_tokens tokens of
- * `choices` choices each (1..64; max_tokens * choices below 2^31) and `experts`
+ * `choices` choices each (1..64; max_tokens * choices at most 2^31 - 4097) and `experts`
  * experts (1..512).  It owns the sort's counters (at most 264 KiB).  All calls
  * must be made with the plan's device current (EBAG_EINVAL otherwise).  One
  * sort may be in flight per plan, checked as the forward's is (EBAG_EBUSY);

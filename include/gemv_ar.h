@@ -169,7 +169,7 @@ void gemv_ar_destroy(gemv_ar_t h);
 typedef struct gemv_ar_q4_plan* gemv_ar_q4_t;
 
 /* Create a plan on the current HIP device for E = experts (1..512) matrices
- * of M rows and K columns (M * K below 2^40, both below 2^31), group a positive
+ * of M rows and K columns (M * K at most 2^40, M below 2^31, K at most 2^31 - 4097), group a positive
  * multiple of 32, glu 0 or 1 (M even).  It owns no device memory; its calls
  * share nothing, may run on any stream and can be captured into a graph.  They
  * must be made with the plan's device current (EBAG_EINVAL otherwise). */

@@ -602,7 +602,7 @@ int ebag_a2a_moe_create(ebag_a2a_moe_t* out, int64_t max_tokens, int32_t choices
   if (choices < 1 || choices > kMaxChoices) return fail(EBAG_EINVAL, "choices=%d outside [1, %d]", choices, kMaxChoices);
   if (experts < 1 || experts > kMaxExperts) return fail(EBAG_EINVAL, "experts=%d outside [1, %d]", experts, kMaxExperts);
   if (max_tokens < 0 || max_tokens > (INT_MAX - kSortThreads * kSortBatches) / choices)
-    return fail(EBAG_EINVAL, "max_tokens=%lld: max_tokens * choices must be below 2^31", (long long)max_tokens);
+    return fail(EBAG_EINVAL, "max_tokens=%lld: max_tokens * choices must be at most 2^31 - 4097", (long long)max_tokens);
   ebag_a2a_moe_plan* h = new (std::nothrow) ebag_a2a_moe_plan();
   if (!h) return fail(EBAG_ENOMEM, "host allocation failed");
   h->max_tokens = max_tokens;
