@@ -414,9 +414,18 @@ __global__ __launch_bounds__(kRowThreads) void moe_combine_backward_kernel(const
         for (int u = 0; u < U; ++u) {
           float g[T::N], s[T::N];
           T::widen(y[i][u], g);
-          // Elements that the last vector repeats count once, whatever they hold: 0 in place of one factor alone would
-          // make an infinity in the other a NaN.
-          const bool repeats = a.twice && v + u * at.lanes == a.vecs - 1;
+          // Elements that the last vector repeats count once, whatever they hold: both factors are 0, as 0 in place of one
+          // would make an infinity in the other a NaN.
+          float d[T::N];
+#pragma unroll
+          for (int n = 0; n < T::N; ++n) d[n] = f[u][n];
+          if (a.twice && v + u * at.lanes == a.vecs - 1) {
+#pragma unroll
+            for (int n = 0; n < T::N; ++n) {
+              d[n] = n < a.twice ? 0.f : d[n];
+              g[n] = n < a.twice ? 0.f : g[n];
+            }
+          }
 #pragma unroll
           for (int n = 0; n < T::N; ++n) {
             // Rounded to fp32 and then to the type, in every instance: the empty statement keeps the compiler from an
@@ -424,16 +433,7 @@ __global__ __launch_bounds__(kRowThreads) void moe_combine_backward_kernel(const
             s[n] = w * f[u][n];
             asm("" : "+v"(s[n]));
             s[n] = p < kept ? s[n] : 0.f;
-          }
-          if (p < kept) {
-            if (repeats) {
-#pragma unroll
-              for (int n = 0; n < T::N; ++n)
-                if (n >= a.twice) dot[i] = __builtin_fmaf(f[u][n], g[n], dot[i]);
-            } else {
-#pragma unroll
-              for (int n = 0; n < T::N; ++n) dot[i] = __builtin_fmaf(f[u][n], g[n], dot[i]);
-            }
+            if (p < kept) dot[i] = __builtin_fmaf(d[n], g[n], dot[i]);
           }
           if (v + u * at.lanes < a.vecs) store_row<STREAM == BOTH>(a.out + p * a.ld_out + byte_of(a, v + u * at.lanes), T::narrow(s));
         }
