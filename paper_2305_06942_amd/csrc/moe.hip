@@ -207,7 +207,7 @@ struct RowArgs {
 //
 // All of these move bytes only: 606 MB dispatched in 102 us (5.9 TB/s; a large copy
 // reaches 5.1, a fill 6.9), combined in 115 us, and combine's gradients read and write
-// 1.2 GB in 225 us.
+// 1.2 GB in 228 us.
 template <bool WHOLE>
 struct Place {
   int64_t token;

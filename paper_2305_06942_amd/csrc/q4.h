@@ -52,7 +52,8 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 // most that way, so fp32 loses 3 bits (fp16) or 4 (bf16) of its 24: fewer than the
 // rounding of y to 11 and 8 bits does, and the larger BASE leaves one code of
 // four where it is and saves its shift.  An fp32 y keeps all its bits, so there BASE +
-// zero comes off each code before the products (`centred`; Y32 in the kernels).  fp32 x
+// zero comes off each code before the products (`centred`; Y32 in the kernels; one row x
+// 65536 x 8192: bf16 57 us with a bf16 y, 77 with fp32, fp16 61 and 62).  fp32 x
 // goes as three bf16 parts whose sum is x, bit for bit (but for bits below 2^-133), so
 // its products are exact too.
 template <int DT> struct Q4Type;

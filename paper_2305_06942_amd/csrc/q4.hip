@@ -196,7 +196,11 @@ int launch_few(const gemv_ar_q4_plan* h, Q4Args a, bool y32, hipStream_t stream)
     a.split *= 2;
   // Its turns: as many workgroups as the card's registers hold at a time, `held` to a CU, so that x is staged once and no
   // place runs empty early (gated, 512 of them: 128 experts of 2 x 1024 x 2048, two rows each, with 512 workgroups 52.1
-  // us, 768 55.9, 1024 56.0, 384 61; one fp16 row x 65536 x 8192, 1024 of them: with 1024 56.7, 2048 60.0, 768 65.7).
+  // us, 768 55.9, 1024 56.0, 384 61; 64 experts of 4096 x 2048, four rows each, with 512 57.6, 1024 57.8, 2048 60.8, 256
+  // 68; the same plain, 1024 of them: with 1024 58.6, 2048 58.8, 512 66.5, 256 94; one fp16 row x 65536 x 8192, 1024 of
+  // them: with 1024 56.7, 2048 60.0, 768 65.7).  With experts `slots` is the most tiles that their rows can make: where
+  // many have none, fewer workgroups have work (128 gated experts of 2 x 1024 x 2048 with one row each at random, a third
+  // of them without: 49.5 us, with 1024 workgroups 44.8).
   const int64_t turn_rows = 16 * (waves / a.split);
   const int64_t all_turns = (a.out_rows + turn_rows - 1) / turn_rows;
   const int64_t held = (rt == 2 ? 8 : parts == 3 ? 12 : 16) / waves;
@@ -253,7 +257,8 @@ int launch_tile(const gemv_ar_q4_plan* h, Q4Args a, bool y32, int x_tiles, hipSt
 // rows 280, 141, 129.  One matrix of 8192 x 4096: 64 rows 22, 48, 67; 256 rows 64, 49,
 // 67.)  fp32 x: 16.5 ns; with 32 rows 235 ns and 64 us, or 272 ns and 85 us (one of 4096 x
 // 4096, in us by the two: 64 rows 34, 63; 512 rows 128, 69; 2048 rows 490, 234; with groups
-// of 32 523, 279).  An expert's rows fill their last tile half on average.
+// of 32 523, 279).  bf16 x with an fp32 y takes 1.3 times as long in all three (8192 x 4096, in
+// us: 128 rows 49, 65, 85; 256 rows 92, 67, 86; 512 rows 173, 96, 89).  An expert's rows fill their last tile half on average.
 int launch(const gemv_ar_q4_plan* h, const Q4Args& a, int y_dtype, hipStream_t stream) {
   const bool y32 = y_dtype == EBAG_F32;
   if (h->K >= 1 << 27) return launch_few(h, a, y32, stream);

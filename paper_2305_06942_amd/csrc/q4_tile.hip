@@ -78,9 +78,13 @@ struct Tile {
 // sum is exact, and the other operand is -(BASE + zero) three times.  With fp32 y (Y32) BASE
 // and zero come off the codes; three parts of fp32 x are multiplied with them (2048 x
 // 4096 x 4096: 234 us, 294 TFLOP/s, 880 of the matrix unit's; fp32's own 154).
+// That takes two vector instructions and a half more for every pair of bf16 codes and one for
+// fp16's, and no correction (2048 x 8192 x 4096 with fp32 and 16-bit y: bf16 235 and 158
+// us, fp16 161 and 165).
 //
 // Bound by the latency and the L1 work of its loads: 32768 rows on 64 experts of 4096 x
-// 2048 (550 GFLOP) 710 to 750 us, 750 TFLOP/s; a large bf16 product reaches 1360.  The
+// 2048 (550 GFLOP) 740 us, 745 TFLOP/s, from about the thirtieth launch on (on an idle
+// card the first ones take up to 1000); a large bf16 product reaches 1360.  The
 // same loads from one hot place 630 us, without loads 494, of which a ninth is the
 // correction.  512 weight rows to a workgroup (one on a CU instead of two) take 921 us;
 // 32 rows of x 1073.  256 x 64 is what the registers hold twice on a CU: 128 of 256 of a
