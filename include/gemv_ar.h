@@ -176,7 +176,7 @@ typedef struct gemv_ar_q4_plan* gemv_ar_q4_t;
 int gemv_ar_q4_create(gemv_ar_q4_t* out, int64_t M, int64_t K, int32_t group, int32_t dtype, int32_t experts,
                       int32_t glu);
 
-/* Round weights w [E][M][K] (contiguous, of dtype, below 2^127) to 4 bits.  With
+/* Round weights w [E][M][K] (contiguous, of dtype, finite, below 2^127) to 4 bits.  With
  * zeros, a group's scale is (max(w, 0) - min(w, 0)) / 15 and its zero the code
  * of 0; without, the scale is max|w| / 7 and the zero 8.  The scale is rounded
  * to dtype first and a code is the nearest to w / scale (halves to even) from

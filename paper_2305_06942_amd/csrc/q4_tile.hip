@@ -76,11 +76,11 @@ struct Tile {
 // correction, -(BASE + zero) * (sum of x), is one more matrix instruction, in bf16: the
 // sum of x is found when x is staged and lies behind its row in three parts, whose
 // sum is exact, and the other operand is -(BASE + zero) three times.  With fp32 y (Y32) BASE
-// and zero come off the codes; three parts of fp32 x are multiplied with them (2048 x
-// 4096 x 4096: 234 us, 294 TFLOP/s, 880 of the matrix unit's; fp32's own 154).
-// That takes two vector instructions and a half more for every pair of bf16 codes and one for
-// fp16's, and no correction (2048 x 8192 x 4096 with fp32 and 16-bit y: bf16 235 and 158
-// us, fp16 161 and 165).
+// and zero come off the codes, three vector instructions for every pair of bf16 codes and
+// one for fp16's, and there is no correction (2048 x 8192 x 4096 with fp32 and 16-bit y:
+// bf16 235 and 158 us, fp16 161 and 165); three parts of fp32 x are multiplied with the
+// codes (2048 x 4096 x 4096: 234 us, 294 TFLOP/s, 880 of the matrix unit's; fp32's own
+// 154).
 //
 // Bound by the latency and the L1 work of its loads: 32768 rows on 64 experts of 4096 x
 // 2048 (550 GFLOP) 740 us, 745 TFLOP/s, from about the thirtieth launch on (on an idle
