@@ -447,6 +447,61 @@ int ebag_a2a_moe_combine_backward(ebag_a2a_moe_t h, const void* dout, int64_t ld
                                   const int32_t* pos, const float* weights, void* dys, int64_t lddys, float* dweights,
                                   hipStream_t stream);
 
+/*
+ * The router of a mixture-of-experts layer, on the same plan: the choices that
+ * the sort takes, their weights for combine, and what keeps the experts' loads
+ * even while a model is trained.
+ *
+ * Token n has a logit l[n][e] for every expert.  Its choices are the experts of
+ * the largest scores l[n][e] + bias[e] (one fp32 addition; bias NULL: 0), the
+ * largest first, equal ones from the lowest number on; a score of -inf or NaN is
+ * no choice.  Choices that are left over are -1, with weight 0.  With p[n] the
+ * softmax of l[n] (the bias has no part in it) and normalise = 0 a weight is
+ * p[n][e] of its expert; with 1 the softmax over the chosen experts' logits alone.
+ *
+ *   T          tokens that count: live[n] is not 0 (NULL: all) and a logit of
+ *              theirs is above -inf.  The others have choices of -1 and weights
+ *              of 0, and logits of tokens that are not live are not read
+ *   counts[e]  choices of expert e; counts[experts] = T
+ *   sums[e]    sum over them of p[n][e]; sums[experts] the sum of z[n]^2, z the
+ *              logarithm of the sum of l[n]'s exponentials
+ *   losses[0]  experts / (choices * T^2) * sum_e counts[e] * sums[e]: the balance
+ *              loss, 1 where every expert has its share
+ *   losses[1]  sums[experts] / T; both are 0 where T is 0
+ *
+ * The gradient takes counts as constants.  Counts of several devices, added up,
+ * give the gradient of the loss over all their tokens.
+ *
+ * Logits are fp32, fp16 or bf16, row n at element n * ldl, aligned to the element
+ * only; all else is computed in fp32.  A NaN or +inf logit makes its own token's
+ * probabilities NaN, and with them its weights, unless normalise is 1 and it is
+ * not chosen, the totals, and its row of the gradient.  Results are the same bits
+ * on every run.  Outputs must not overlap inputs.
+ */
+
+/* fp32 elements of `work` that a call with totals needs, for any number of tokens. */
+int64_t ebag_a2a_moe_choose_work(ebag_a2a_moe_t h);
+
+/* Choose: logits [tokens][experts] -> ids int32 and weights fp32 [tokens][choices].
+ * counts int32 [experts + 1], sums fp32 [experts + 1], losses fp32 [2] and the
+ * scratch memory work go together and may all be NULL: one launch then, two with
+ * them where there are more than a few tokens.  Calls share nothing but a work
+ * that the caller gives to several, which must not run at the same time; all can be
+ * captured into a graph. */
+int ebag_a2a_moe_choose(ebag_a2a_moe_t h, const void* logits, int64_t ldl, int32_t dtype, int64_t tokens,
+                        const float* bias, const uint8_t* live, int32_t normalise, int32_t* ids, float* weights,
+                        int32_t* counts, float* sums, float* losses, float* work, hipStream_t stream);
+
+/* Gradient of the weights and of both losses: dlogits [tokens][experts] of the
+ * logits' type, zeros for tokens that do not count.  live and normalise as they were
+ * for the choice, ids its choices (ones outside [0, experts) are none).  dweights fp32
+ * [tokens][choices] may be NULL (none), and dlosses, fp32 [2] on the device, too; counts
+ * are needed with dlosses only. */
+int ebag_a2a_moe_choose_backward(ebag_a2a_moe_t h, const void* logits, int64_t ldl, int32_t dtype, int64_t tokens,
+                                 const uint8_t* live, int32_t normalise, const int32_t* ids, const float* dweights,
+                                 const int32_t* counts, const float* dlosses, void* dlogits, int64_t lddl,
+                                 hipStream_t stream);
+
 /* Release the plan's device memory.  NULL is ignored. */
 void ebag_a2a_moe_destroy(ebag_a2a_moe_t h);
 

@@ -95,6 +95,11 @@ _SIGS = {
                               ctypes.c_int64, _P], ctypes.c_int),
     "ebag_a2a_moe_combine_backward": ([_P, _P, ctypes.c_int64, _P, ctypes.c_int64, ctypes.c_int64, ctypes.c_int32,
                                        ctypes.c_int64, _P, _P, _P, _P, ctypes.c_int64, _P, _P], ctypes.c_int),
+    "ebag_a2a_moe_choose_work": ([_P], ctypes.c_int64),
+    "ebag_a2a_moe_choose": ([_P, _P, ctypes.c_int64, ctypes.c_int32, ctypes.c_int64, _P, _P, ctypes.c_int32, _P, _P, _P, _P,
+                             _P, _P, _P], ctypes.c_int),
+    "ebag_a2a_moe_choose_backward": ([_P, _P, ctypes.c_int64, ctypes.c_int32, ctypes.c_int64, _P, ctypes.c_int32, _P, _P, _P,
+                                      _P, _P, ctypes.c_int64, _P], ctypes.c_int),
     "ebag_a2a_moe_destroy": ([_P], None),
     "gemv_ar_default_opts": ([_P], ctypes.c_int),
     "gemv_ar_create": ([_P, ctypes.c_int32, ctypes.c_int64, _P, ctypes.c_int32, _P], ctypes.c_int),
@@ -488,6 +493,8 @@ class MoePerm:
         import torch
         self.choices, self.experts = int(choices), int(experts)
         self._i32, self._f32 = torch.int32, torch.float32
+        self._flags = (torch.bool, torch.uint8)
+        self.choose_work = 512 * (self.experts + 1)  # ebag_a2a_moe_choose_work
 
     def _places(self, offsets, pos, *weights) -> int:
         """Checks what every call over rows shares; the number of tokens.
@@ -503,6 +510,52 @@ class MoePerm:
             _refuse((offsets, "offsets", I32, 4 * (self.experts + 1)), (pos, "pos", I32, 0),
                     *((w, what, F32, 4 * n) for w, what in zip(weights, ("weights", "dweights"))))
         return tokens
+
+    def _live(self, live, n):
+        """live: None, or one truth value of a byte for each of n tokens."""
+        if live is not None and not (live.dtype in self._flags and live.is_cuda and live.is_contiguous() and live.numel() >= n):
+            _refuse((live, "live", ("bool", "uint8"), n))
+        return _addr(live)
+
+    def choose(self, logits, ids, weights, counts=None, sums=None, losses=None, work=None, bias=None, live=None,
+               normalise=True, stream=None):
+        """ebag_a2a_moe_choose.  counts, sums, losses and work (float32
+        [choose_work]) go together; live: bool or uint8 [tokens]."""
+        n, k, E = logits.shape[0], self.choices, self.experts
+        pl, ldl, kind = _matrix(logits, n, E, None, "logits")
+        ok = _fit(ids, self._i32, n * k) and _fit(weights, self._f32, n * k) and (bias is None or _fit(bias, self._f32, E))
+        totals = counts is not None or sums is not None or losses is not None or work is not None
+        if totals:
+            if counts is None or sums is None or losses is None or work is None:
+                raise ValueError("counts, sums, losses and work go together: all of them or none")
+            ok = (ok and _fit(counts, self._i32, E + 1) and _fit(sums, self._f32, E + 1) and _fit(losses, self._f32, 2) and
+                  _fit(work, self._f32, self.choose_work))
+        if not ok:
+            _refuse((ids, "ids", I32, 4 * n * k), (weights, "weights", F32, 4 * n * k), (bias, "bias", F32, 4 * E),
+                    (counts, "counts", I32, 4 * (E + 1)), (sums, "sums", F32, 4 * (E + 1)), (losses, "losses", F32, 8),
+                    (work, "work", F32, 4 * self.choose_work))
+        _check(self._lib.ebag_a2a_moe_choose(self._h, pl, ldl, ROW_TYPES[kind], n, _addr(bias), self._live(live, n),
+                                             int(bool(normalise)), ids.data_ptr(), weights.data_ptr(), _addr(counts),
+                                             _addr(sums), _addr(losses), _addr(work), _stream(stream)))
+
+    def choose_backward(self, logits, ids, dweights, dlogits, counts=None, dlosses=None, live=None, normalise=True,
+                        stream=None):
+        """ebag_a2a_moe_choose_backward.  dweights may be None, and dlosses (then
+        counts, too)."""
+        n, k, E = logits.shape[0], self.choices, self.experts
+        pl, ldl, kind = _matrix(logits, n, E, None, "logits")
+        pd, ldd, _ = _matrix(dlogits, n, E, kind, "dlogits")
+        ok = dweights is None or (ids is not None and _fit(ids, self._i32, n * k) and _fit(dweights, self._f32, n * k))
+        if dlosses is not None:
+            ok = ok and _fit(dlosses, self._f32, 2) and counts is not None and _fit(counts, self._i32, E + 1)
+        if not ok:
+            if dweights is not None and ids is None or dlosses is not None and counts is None:
+                raise ValueError("dweights need ids, dlosses need counts")
+            _refuse((ids, "ids", I32, 4 * n * k), (dweights, "dweights", F32, 4 * n * k), (dlosses, "dlosses", F32, 8),
+                    (counts, "counts", I32, 4 * (E + 1)))
+        _check(self._lib.ebag_a2a_moe_choose_backward(self._h, pl, ldl, ROW_TYPES[kind], n, self._live(live, n),
+                                                      int(bool(normalise)), _addr(ids), _addr(dweights), _addr(counts),
+                                                      _addr(dlosses), pd, ldd, _stream(stream)))
 
     def sort(self, experts_of, offsets, pos, src, stream=None):
         n, i32 = experts_of.numel(), self._i32

@@ -9,13 +9,12 @@
 #include "ebag_a2a.h"
 #include "in_flight.h"
 #include "lanes.h"
+#include "moe.h"
 #include "vec16.h"
 
 using namespace ebag;
 
 namespace {
-
-constexpr int kMaxChoices = 64, kMaxExperts = 512;
 
 // ------------------------------------------------------------------- sort
 //
@@ -507,18 +506,6 @@ row_fn pick(Which which, bool whole, int stream) {
 
 int hipf(hipError_t e, const char* what) { return fail(EBAG_EHIP, "%s: %s", what, hipGetErrorString(e)); }
 
-}  // namespace
-
-struct ebag_a2a_moe_plan {
-  int device = 0;
-  int64_t max_tokens = 0;
-  int32_t choices = 0, experts = 0;
-  uint32_t* d_counts = nullptr;
-  InFlight sort;
-};
-
-namespace {
-
 void free_moe(ebag_a2a_moe_plan* h) {
   if (!h) return;
   if (h->sort.done) (void)hipEventDestroy(h->sort.done);
@@ -526,20 +513,10 @@ void free_moe(ebag_a2a_moe_plan* h) {
   delete h;
 }
 
-int check_plan(ebag_a2a_moe_plan* h, int64_t tokens) {
-  if (!h) return fail(EBAG_EINVAL, "null plan");
-  int dev = -1;
-  if (hipGetDevice(&dev) != hipSuccess || dev != h->device)
-    return fail(EBAG_EINVAL, "the plan belongs to device %d, but device %d is current", h->device, dev);
-  if (tokens < 0 || tokens > h->max_tokens)
-    return fail(EBAG_EINVAL, "tokens=%lld outside [0, max_tokens=%lld]", (long long)tokens, (long long)h->max_tokens);
-  return EBAG_OK;
-}
-
 // Checks a row call's shape and fills what all of them share.
 int row_args(ebag_a2a_moe_plan* h, int64_t dim, int32_t dtype, int64_t tokens, const int32_t* offsets,
              const int32_t* pos, RowArgs* a) {
-  if (int rc = check_plan(h, tokens)) return rc;
+  if (int rc = check_moe_plan(h, tokens)) return rc;
   if (dtype != EBAG_F32 && dtype != EBAG_F16 && dtype != EBAG_BF16) return fail(EBAG_EINVAL, "bad dtype %d", (int)dtype);
   if (dim < 1 || dim > INT_MAX / 4) return fail(EBAG_EINVAL, "dim=%lld outside [1, 2^29)", (long long)dim);
   if (tokens && (!offsets || !pos)) return fail(EBAG_EINVAL, "null offsets or pos");
@@ -622,7 +599,7 @@ int ebag_a2a_moe_create(ebag_a2a_moe_t* out, int64_t max_tokens, int32_t choices
 
 int ebag_a2a_moe_sort(ebag_a2a_moe_t h, const int32_t* experts_of, int64_t tokens, int32_t* offsets, int32_t* pos,
                       int32_t* src, hipStream_t stream) {
-  if (int rc = check_plan(h, tokens)) return rc;
+  if (int rc = check_moe_plan(h, tokens)) return rc;
   if (!offsets || (tokens && (!experts_of || !pos || !src))) return fail(EBAG_EINVAL, "null experts_of, offsets, pos or src");
   SortArgs a{};
   a.experts_of = experts_of;

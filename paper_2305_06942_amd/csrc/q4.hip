@@ -165,13 +165,6 @@ int fill_args(const gemv_ar_q4_plan* h, const uint8_t* codes, const void* scales
   return EBAG_OK;
 }
 
-// Most tiles of `cols` rows that `rows` rows of `experts` experts and the
-// dropped rows behind them can make.
-int64_t most_tiles(int64_t rows, int64_t experts, int64_t cols) {
-  const int64_t n = (rows + (experts + 1) * (cols - 1)) / cols;
-  return n < rows ? n : rows;
-}
-
 int launch_few(const gemv_ar_q4_plan* h, Q4Args a, bool y32, hipStream_t stream) {
   const int rt = h->glu ? 2 : 1, parts = h->dtype == EBAG_F32 ? 3 : 1;
   const bool whole = h->group % 128 == 0;
