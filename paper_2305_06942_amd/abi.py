@@ -494,7 +494,7 @@ class MoePerm:
         self.choices, self.experts = int(choices), int(experts)
         self._i32, self._f32 = torch.int32, torch.float32
         self._flags = (torch.bool, torch.uint8)
-        self.choose_work = 512 * (self.experts + 1)  # ebag_a2a_moe_choose_work
+        self.choose_work = 32 + 512 * (self.experts + 1)  # ebag_a2a_moe_choose_work
 
     def _places(self, offsets, pos, *weights) -> int:
         """Checks what every call over rows shares; the number of tokens.

@@ -15,10 +15,11 @@ using namespace ebag;
 
 namespace {
 
-// 2^k lanes (4 to 64) have a token, V of its logits each, four neighbouring ones at
-// a time: logit (u * lanes + lane) * 4 + c in place 4 u + c.
-constexpr int kLeastLanes = 4;
+// L lanes (4 to 64) have a token, V of its logits each, four neighbouring ones at
+// a time: logit (u * L + lane) * 4 + c in place 4 u + c.
 constexpr int kMostParts = 256;   // workgroups whose totals are joined
+constexpr int kJoinColumns = 32;  // of a workgroup that joins them
+constexpr int kMostJoins = (kMaxExperts + kJoinColumns) / kJoinColumns;
 
 struct ChooseArgs {
   const char* logits;
@@ -32,37 +33,59 @@ struct ChooseArgs {
   int32_t* counts;          // nullptr: no totals
   float* sums;
   float* losses;
-  float* work;              // sums [workgroups][experts + 1], then counts
+  float* work;              // of the joining workgroups: how many are done, their parts of the balance; then sums
+                            // [workgroups][experts + 1], then counts
   int64_t ld, ld_out;       // bytes
   int64_t tokens;
   int32_t E, k;
-  int32_t lanes, lanes_shift;
   int32_t turns;            // tokens of a group of lanes
+  int32_t dtype;
   int32_t normalise;
   float coef;               // experts / choices
 };
 
+__device__ __forceinline__ float* parts_of(float* work) { return work + 32; }
+static_assert(1 + kMostJoins <= 32, "");
+
 __device__ __forceinline__ double join(uint32_t lo, uint32_t hi) { return __hiloint2double((int)hi, (int)lo); }
 
 template <int CTRL>
-__device__ __forceinline__ double larger_dpp(double v) {
-  const uint32_t lo = __builtin_amdgcn_update_dpp(0, __double2loint(v), CTRL, 0xf, 0xf, true);
-  const uint32_t hi = __builtin_amdgcn_update_dpp(0, __double2hiint(v), CTRL, 0xf, 0xf, true);
-  return __builtin_fmax(v, join(lo, hi));
+__device__ __forceinline__ double move_dpp(double v) {
+  return join(__builtin_amdgcn_update_dpp(0, __double2loint(v), CTRL, 0xf, 0xf, true),
+              __builtin_amdgcn_update_dpp(0, __double2hiint(v), CTRL, 0xf, 0xf, true));
 }
 
-// The largest over 2^k neighbouring lanes, 4 at least, in each of them.
-__device__ __forceinline__ double largest(double v, int lanes) {
-  v = larger_dpp<0xB1>(v);
-  v = larger_dpp<0x4E>(v);
-  if (lanes >= 8) v = larger_dpp<0x141>(v);
-  if (lanes >= 16) v = larger_dpp<0x140>(v);
-  if (lanes >= 32) {
+// What a lane of the other half of 2 * D lanes has, the same lane in both halves of what
+// follows: lanes of a group hold the same before and after steps 1, 2, ... up to D.
+template <int D>
+__device__ __forceinline__ double other(double v, int lane) {
+  if constexpr (D == 1) return move_dpp<0xB1>(v);    // quad_perm 1 0 3 2
+  if constexpr (D == 2) return move_dpp<0x4E>(v);    // quad_perm 2 3 0 1
+  if constexpr (D == 4) return move_dpp<0x141>(v);   // row_half_mirror
+  if constexpr (D == 8) return move_dpp<0x140>(v);   // row_mirror
+  if constexpr (D == 16) {
+    const u32x2 lo = __builtin_amdgcn_permlane16_swap(__double2loint(v), __double2loint(v), false, false);
+    const u32x2 hi = __builtin_amdgcn_permlane16_swap(__double2hiint(v), __double2hiint(v), false, false);
+    return lane & 16 ? join(lo[0], hi[0]) : join(lo[1], hi[1]);
+  }
+  const u32x2 lo = __builtin_amdgcn_permlane32_swap(__double2loint(v), __double2loint(v), false, false);
+  const u32x2 hi = __builtin_amdgcn_permlane32_swap(__double2hiint(v), __double2hiint(v), false, false);
+  return lane & 32 ? join(lo[0], hi[0]) : join(lo[1], hi[1]);
+}
+
+// The largest over L neighbouring lanes, in each of them.
+template <int L>
+__device__ __forceinline__ double largest(double v) {
+  v = __builtin_fmax(v, move_dpp<0xB1>(v));
+  v = __builtin_fmax(v, move_dpp<0x4E>(v));
+  if constexpr (L >= 8) v = __builtin_fmax(v, move_dpp<0x141>(v));
+  if constexpr (L >= 16) v = __builtin_fmax(v, move_dpp<0x140>(v));
+  if constexpr (L >= 32) {
     const u32x2 lo = __builtin_amdgcn_permlane16_swap(__double2loint(v), __double2loint(v), false, false);
     const u32x2 hi = __builtin_amdgcn_permlane16_swap(__double2hiint(v), __double2hiint(v), false, false);
     v = __builtin_fmax(join(lo[0], hi[0]), join(lo[1], hi[1]));
   }
-  if (lanes >= 64) {
+  if constexpr (L >= 64) {
     const u32x2 lo = __builtin_amdgcn_permlane32_swap(__double2loint(v), __double2loint(v), false, false);
     const u32x2 hi = __builtin_amdgcn_permlane32_swap(__double2hiint(v), __double2hiint(v), false, false);
     v = __builtin_fmax(join(lo[0], hi[0]), join(lo[1], hi[1]));
@@ -81,14 +104,22 @@ __device__ __forceinline__ bool is_none(double key) { return (uint32_t)__double2
 
 __device__ __forceinline__ double key_of(float score, int e) {
   const double d = (double)(score + 0.f);
-  uint32_t hi = (uint32_t)__double2hiint(d), lo = (uint32_t)__double2loint(d);
-  if (score == __builtin_inff()) hi = 0x47f00000u;
-  lo |= (int32_t)hi < 0 ? (uint32_t)e : kNumber - (uint32_t)e;
-  return score > -__builtin_inff() ? join(lo, hi) : none();
+  const int hi = __double2hiint(d);
+  const int lo = __double2loint(d) | (e ^ (~(hi >> 31) & (int)kNumber));
+  return score > -__builtin_inff() ? join((uint32_t)lo, (uint32_t)(hi < 0x47f00000 ? hi : 0x47f00000)) : none();
 }
 __device__ __forceinline__ int number_of(double key) {
   const uint32_t at = (uint32_t)__double2loint(key) & kNumber;
-  return (int)(__double2hiint(key) < 0 ? at : kNumber - at);
+  return is_none(key) ? -1 : (int)(__double2hiint(key) < 0 ? at : kNumber - at);
+}
+__device__ __forceinline__ float score_of(double key) {
+  return (float)join((uint32_t)__double2loint(key) & ~kNumber, (uint32_t)__double2hiint(key));
+}
+
+__device__ __forceinline__ void order(double& a, double& b) {
+  const double x = a, y = b;
+  a = __builtin_fmax(x, y);
+  b = __builtin_fmin(x, y);
 }
 
 // Sorts V keys downwards (Batcher's odd-even merge sort).
@@ -102,180 +133,221 @@ __device__ __forceinline__ void sort_down(double* key) {
       for (int j = q % p; j + q < V; j += 2 * q)
 #pragma unroll
         for (int i = 0; i < q; ++i)
-          if (i + j + q < V && (i + j) / (2 * p) == (i + j + q) / (2 * p)) {
-            const double a = key[i + j], b = key[i + j + q];
-            key[i + j] = __builtin_fmax(a, b);
-            key[i + j + q] = __builtin_fmin(a, b);
-          }
+          if (i + j + q < V && (i + j) / (2 * p) == (i + j + q) / (2 * p)) order(key[i + j], key[i + j + q]);
 }
 
-template <int DT>
-__device__ __forceinline__ float logit_at(const char* row, int e) {
-  return Type<DT>::widen(reinterpret_cast<const typename Type<DT>::elt*>(row)[e]);
+// The K largest of two lists of K sorted downwards, sorted: the larger of one's first and the
+// other's last and so on are those K in an order that rises once and falls once.
+template <int K>
+__device__ __forceinline__ void merge_down(double* a, const double* b) {
+#pragma unroll
+  for (int i = 0; i < K; ++i) a[i] = __builtin_fmax(a[i], b[K - 1 - i]);
+#pragma unroll
+  for (int d = K / 2; d >= 1; d /= 2)
+#pragma unroll
+    for (int i = 0; i < K; ++i)
+      if (!(i & d)) order(a[i], a[i + d]);
+}
+
+template <int D, int K>
+__device__ __forceinline__ void merge_lanes(double* key, int lane) {
+  double theirs[K];
+#pragma unroll
+  for (int i = 0; i < K; ++i) theirs[i] = other<D>(key[i], lane);
+  merge_down<K>(key, theirs);
+}
+
+__device__ __forceinline__ float logit_at(const ChooseArgs& a, const char* row, int e) {
+  if (a.dtype == EBAG_F32) return reinterpret_cast<const float*>(row)[e];
+  const uint16_t v = reinterpret_cast<const uint16_t*>(row)[e];
+  return a.dtype == EBAG_F16 ? (float)__builtin_bit_cast(_Float16, v) : __uint_as_float((uint32_t)v << 16);
 }
 
 typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
 
 // A lane's V logits; -inf behind the last expert.
-template <int DT, int V>
-__device__ __forceinline__ void load_logits(const ChooseArgs& a, const char* row, int lane, float* x) {
+template <int V, int L>
+__device__ __forceinline__ void load_logits(int dtype, int E, const char* row, int lane, float* x) {
+  uint32_t raw[V];
+  if (dtype == EBAG_F32) {
+#pragma unroll
+    for (int u = 0; u < V / 4; ++u) {
+      const int e = (u * L + lane) * 4;
+      if (e + 4 <= E) {
+        const vec16 v = load16(row + e * 4);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) raw[4 * u + c] = v[c];
+      } else {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) raw[4 * u + c] = e + c < E ? reinterpret_cast<const uint32_t*>(row)[e + c] : 0xff800000u;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) x[i] = __uint_as_float(raw[i]);
+    return;
+  }
+  const uint32_t below = dtype == EBAG_F16 ? 0xfc00u : 0xff80u;
 #pragma unroll
   for (int u = 0; u < V / 4; ++u) {
-    const int e = (u * a.lanes + lane) * 4;
-    if (e + 4 <= a.E) {
-      if constexpr (DT == 0) {
-        Type<0>::widen(load16(row + e * 4), x + 4 * u);
-      } else {
-        const u32x2_any two = *reinterpret_cast<const u32x2_any*>(row + e * 2);
-        float f[8];
-        Type<DT>::widen(vec16{two[0], two[1], 0, 0}, f);
+    const int e = (u * L + lane) * 4;
+    if (e + 4 <= E) {
+      const u32x2_any two = *reinterpret_cast<const u32x2_any*>(row + e * 2);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) x[4 * u + c] = f[c];
-      }
+      for (int c = 0; c < 4; ++c) raw[4 * u + c] = c & 1 ? two[c / 2] >> 16 : two[c / 2] & 0xffffu;
     } else {
 #pragma unroll
-      for (int c = 0; c < 4; ++c) x[4 * u + c] = e + c < a.E ? logit_at<DT>(row, e + c) : -__builtin_inff();
+      for (int c = 0; c < 4; ++c) raw[4 * u + c] = e + c < E ? reinterpret_cast<const uint16_t*>(row)[e + c] : below;
     }
+  }
+  if (dtype == EBAG_F16) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) x[i] = (float)__builtin_bit_cast(_Float16, (uint16_t)raw[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) x[i] = __uint_as_float(raw[i] << 16);
   }
 }
 
 // exp(x - top) of a lane's logits in place of them; their sum over the token's lanes.
-template <int V>
-__device__ __forceinline__ float exponentials(float* x, float top, int lanes) {
+template <int V, int L>
+__device__ __forceinline__ float exponentials(float* x, float top) {
   float sum = 0.f;
 #pragma unroll
   for (int i = 0; i < V; ++i) {
     x[i] = __expf(x[i] - top);
     sum += x[i];
   }
-  return sum_lanes(sum, lanes);
+  return sum_lanes(sum, L);
 }
 
-template <int V>
-__device__ __forceinline__ float top_of(const float* x, int lanes) {
+template <int V, int L>
+__device__ __forceinline__ float top_of(const float* x) {
   float top = x[0];
 #pragma unroll
   for (int i = 1; i < V; ++i) top = fmaxf(top, x[i]);
-  return max_lanes(top, lanes);
+  return max_lanes(top, L);
 }
 
-// Which lanes of a group and which token.
-struct Group {
-  int lane, own, groups;   // lane of the group; the group's number in the workgroup, of so many
-  __device__ __forceinline__ Group(const ChooseArgs& a) {
-    lane = threadIdx.x & (a.lanes - 1);
-    own = threadIdx.x >> a.lanes_shift;
-    groups = blockDim.x >> a.lanes_shift;
-  }
-};
-
-// Losses of the totals in LDS (sums and counts of experts + 1 each), and the totals to where they belong.
-__device__ void finish(const ChooseArgs& a, const float* sums, const int32_t* counts, float* waves) {
-  const float T = (float)counts[a.E];
-  float part = 0.f;
-  for (int e = threadIdx.x; e <= a.E; e += blockDim.x) {
-    a.sums[e] = sums[e];
-    a.counts[e] = counts[e];
-    if (e < a.E && T > 0.f) part += (float)counts[e] / T * (sums[e] / T);
-  }
-  part = sum_lanes(part, 64);
-  if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = part;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    float all = 0.f;
-    for (unsigned w = 0; w < blockDim.x / 64; ++w) all += waves[w];
-    a.losses[0] = a.coef * all;
-    a.losses[1] = T > 0.f ? sums[a.E] / T : 0.f;
-  }
-}
-
-// The k largest scores of a token: every lane sorts its keys, then the largest of the
-// lanes' first ones is taken off k times.
+// The k largest scores of a token.  MERGE (k up to 8): every lane sorts its keys and keeps
+// eight, and the lanes' lists become one in log2(L) merges, which every lane then has
+// whole.  Otherwise the largest of the lanes' first keys is taken off k times.
 //
 // TOTALS: the probabilities are summed over a workgroup's tokens, in registers, then
 // over its waves in LDS, always in the same order; the choices are counted there
 // with atomics on whole numbers.  One workgroup finishes by itself, several leave
 // their parts to a second launch.
-template <int DT, int V, bool TOTALS>
+template <int V, int L, bool MERGE, bool TOTALS>
 __global__ __launch_bounds__(TOTALS ? 1024 : 256) void choose_kernel(const ChooseArgs a) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
-  const Group g(a);
+  const int lane = threadIdx.x % L, own = threadIdx.x / L, groups = blockDim.x / L;
   const int E = a.E, k = a.k;
-  int2* chosen = reinterpret_cast<int2*>(lds) + g.own * k;  // number and score of each choice
-  int32_t* counts = reinterpret_cast<int32_t*>(lds + (size_t)g.groups * k * 8);  // [E + 1]
-  float* parts = reinterpret_cast<float*>(counts + E + 1);                       // [waves][E + 1]
+  double* chosen = reinterpret_cast<double*>(lds) + own * k;
+  int32_t* counts = reinterpret_cast<int32_t*>(lds + (size_t)groups * k * 8);  // [E + 1]
+  float* parts = reinterpret_cast<float*>(counts + E + 1);                     // [waves][E + 1]
   if (TOTALS) {
     for (int e = threadIdx.x; e <= E; e += blockDim.x) counts[e] = 0;
     __syncthreads();
   }
-  float bias[V], total[V];
+  float total[V];
   float squares = 0.f;
 #pragma unroll
-  for (int i = 0; i < V; ++i) {
-    const int e = ((i / 4) * a.lanes + g.lane) * 4 + i % 4;
-    bias[i] = a.bias && e < E ? a.bias[e] : 0.f;
-    total[i] = 0.f;
-  }
+  for (int i = 0; i < V; ++i) total[i] = 0.f;
   for (int turn = 0; turn < a.turns; ++turn) {
-    const int64_t n = ((int64_t)turn * gridDim.x + blockIdx.x) * g.groups + g.own;
+    const int64_t n = ((int64_t)turn * gridDim.x + blockIdx.x) * groups + own;
     const bool here = n < a.tokens;
     const bool live = here && (!a.live || a.live[n]);
     const char* row = a.logits + n * a.ld;
+    // The compiler keeps a comparison with E for each logit in scalar registers, and spills them, unless E is new here.
+    int E = a.E;
+    asm("" : "+s"(E));
     float x[V];
-    if (live) {
-      load_logits<DT, V>(a, row, g.lane, x);
-    } else {
-#pragma unroll
-      for (int i = 0; i < V; ++i) x[i] = -__builtin_inff();
-    }
     double key[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) key[i] = key_of(x[i] + bias[i], ((i / 4) * a.lanes + g.lane) * 4 + i % 4);
-    const float top = top_of<V>(x, a.lanes);
+    for (int i = 0; i < V; ++i) x[i] = -__builtin_inff();
+    if (live) load_logits<V, L>(a.dtype, E, row, lane, x);
+    if (a.bias) {
+      float score[V];
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const int e = (i / 4 * L + lane) * 4 + i % 4;
+        score[i] = x[i] + a.bias[e < E ? e : E - 1];
+      }
+#pragma unroll
+      for (int i = 0; i < V; ++i) key[i] = key_of(score[i], (i / 4 * L + lane) * 4 + i % 4);
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i) key[i] = key_of(x[i], (i / 4 * L + lane) * 4 + i % 4);
+    }
+    const float top = top_of<V, L>(x);
     const bool counted = top > -__builtin_inff();
-    const float sum = exponentials<V>(x, counted ? top : 0.f, a.lanes);
+    const float sum = exponentials<V, L>(x, counted ? top : 0.f);
     if (TOTALS && counted) {
       const float inv = 1.f / sum;
 #pragma unroll
       for (int i = 0; i < V; ++i) total[i] = __builtin_fmaf(x[i], inv, total[i]);
       const float lse = top + logf(sum);
       squares = __builtin_fmaf(lse, lse, squares);
-      if (g.lane == 0) atomicAdd(&counts[E], 1);
     }
-    sort_down<V>(key);
-    for (int j = 0; j < k; ++j) {
-      const double best = largest(key[0], a.lanes);
-      const bool mine = key[0] == best;
+    if (TOTALS) {
+      const uint64_t some = __ballot(counted && lane == 0);
+      if ((threadIdx.x & 63) == 0) atomicAdd(&counts[E], (int)__popcll(some));
+    }
+    if constexpr (MERGE) {
+      constexpr int K = 8;
+      sort_down<K>(key);
+      if constexpr (V > K) {
+        sort_down<K>(key + K);
+        merge_down<K>(key, key + K);
+      }
+      merge_lanes<1, K>(key, lane);
+      merge_lanes<2, K>(key, lane);
+      if constexpr (L >= 8) merge_lanes<4, K>(key, lane);
+      if constexpr (L >= 16) merge_lanes<8, K>(key, lane);
+      if constexpr (L >= 32) merge_lanes<16, K>(key, threadIdx.x);
+      if constexpr (L >= 64) merge_lanes<32, K>(key, threadIdx.x);
 #pragma unroll
-      for (int i = 0; i + 1 < V; ++i) key[i] = mine ? key[i + 1] : key[i];
-      key[V - 1] = mine ? none() : key[V - 1];
-      if (g.lane == 0) {
-        const uint32_t hi = (uint32_t)__double2hiint(best), lo = (uint32_t)__double2loint(best) & ~kNumber;
-        chosen[j] = is_none(best) || !counted ? int2{-1, 0} : int2{number_of(best), (int)__float_as_uint((float)join(lo, hi))};
+      for (int j = 0; j < K; ++j)
+        if (lane == j % L && j < k) chosen[j] = key[j];
+    } else {
+      sort_down<V>(key);
+#pragma unroll 1
+      for (int j = 0; j < k; ++j) {
+        const double best = largest<L>(key[0]);
+        const bool mine = key[0] == best;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          double next = i + 1 < V ? key[i + 1] : none();
+          asm("" : "+v"(next));  // a value, not an index to select by
+          key[i] = mine ? next : key[i];
+        }
+        if (lane == 0) chosen[j] = best;
       }
     }
     __builtin_amdgcn_wave_barrier();
-    auto logit = [&](const int2& c) {  // of a choice, without the bias
-      return c.x < 0 ? -__builtin_inff() : a.bias ? logit_at<DT>(row, c.x) : __uint_as_float(c.y);
+    auto logit = [&](double c, int id) {  // of a choice, without the bias
+      return a.bias ? logit_at(a, row, id) : score_of(c);
     };
     float from = top, over = sum;
     if (a.normalise) {
       from = -__builtin_inff();
-      for (int j = g.lane; j < k; j += a.lanes) from = fmaxf(from, logit(chosen[j]));
-      from = max_lanes(from, a.lanes);
-      over = 0.f;
-      for (int j = g.lane; j < k; j += a.lanes) {
-        const int2 c = chosen[j];
-        if (c.x >= 0) over += __expf(logit(c) - from);
+      for (int j = lane; j < k; j += L) {
+        const int id = number_of(chosen[j]);
+        if (id >= 0) from = fmaxf(from, logit(chosen[j], id));
       }
-      over = sum_lanes(over, a.lanes);
+      from = max_lanes(from, L);
+      over = 0.f;
+      for (int j = lane; j < k; j += L) {
+        const int id = number_of(chosen[j]);
+        if (id >= 0) over += __expf(logit(chosen[j], id) - from);
+      }
+      over = sum_lanes(over, L);
     }
-    for (int j = g.lane; j < k; j += a.lanes) {
-      const int2 c = chosen[j];
-      if (TOTALS && c.x >= 0) atomicAdd(&counts[c.x], 1);
+    for (int j = lane; j < k; j += L) {
+      const int id = counted ? number_of(chosen[j]) : -1;
+      if (TOTALS && id >= 0) atomicAdd(&counts[id], 1);
       if (here) {
-        a.ids[n * k + j] = c.x;
-        a.weights[n * k + j] = c.x < 0 ? 0.f : __expf(logit(c) - from) / over;
+        a.ids[n * k + j] = id;
+        a.weights[n * k + j] = id < 0 ? 0.f : __expf(logit(chosen[j], id) - from) / over;
       }
     }
     __builtin_amdgcn_wave_barrier();
@@ -283,101 +355,130 @@ __global__ __launch_bounds__(TOTALS ? 1024 : 256) void choose_kernel(const Choos
   if (!TOTALS) return;
   // Over the groups of a wave, then over the waves.
 #pragma unroll
-  for (int d = 32; d >= kLeastLanes; d /= 2) {
-    if (d < a.lanes) break;
+  for (int d = 32; d >= L; d /= 2) {
 #pragma unroll
     for (int i = 0; i < V; ++i) total[i] += __shfl_xor(total[i], d);
     squares += __shfl_xor(squares, d);
   }
   const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-  if ((threadIdx.x & 63) < a.lanes) {
+  if ((threadIdx.x & 63) < L) {
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      const int e = ((i / 4) * a.lanes + g.lane) * 4 + i % 4;
+      const int e = (i / 4 * L + lane) * 4 + i % 4;
       if (e < E) parts[wave * (E + 1) + e] = total[i];
     }
-    if (g.lane == 0) parts[wave * (E + 1) + E] = squares;
+    if (lane == 0) parts[wave * (E + 1) + E] = squares;
   }
   __syncthreads();
   const bool alone = gridDim.x == 1;
-  float* sums = a.work + (size_t)blockIdx.x * (E + 1);
-  int32_t* numbers = reinterpret_cast<int32_t*>(a.work) + ((size_t)gridDim.x + blockIdx.x) * (E + 1);
+  float* sums = parts_of(a.work) + (size_t)blockIdx.x * (E + 1);
+  int32_t* numbers = reinterpret_cast<int32_t*>(parts_of(a.work)) + ((size_t)gridDim.x + blockIdx.x) * (E + 1);
   for (int e = threadIdx.x; e <= E; e += blockDim.x) {
     float s = 0.f;
     for (int w = 0; w < waves; ++w) s += parts[w * (E + 1) + e];
     if (alone) {
       parts[e] = s;  // no other thread reads this column
+      a.sums[e] = s;
+      a.counts[e] = counts[e];
     } else {
       sums[e] = s;
       numbers[e] = counts[e];
     }
   }
-  if (!alone) return;
+  if (!alone) {
+    if (blockIdx.x == 0 && threadIdx.x == 0) *reinterpret_cast<uint32_t*>(a.work) = 0;  // joining workgroups that are done
+    return;
+  }
   __syncthreads();
-  finish(a, parts, counts, parts + (size_t)waves * (E + 1));
+  if (wave > 0) return;
+  float part = 0.f;
+  for (int e = threadIdx.x; e < E; e += 64) part = __builtin_fmaf((float)counts[e], parts[e], part);
+  part = sum_lanes(part, 64);
+  const float per = counts[E] ? 1.f / (float)counts[E] : 0.f;
+  if (threadIdx.x == 0) {
+    a.losses[0] = a.coef * part * per * per;
+    a.losses[1] = parts[E] * per;
+  }
 }
 
-// The workgroups' totals, summed in their order.  Threads: `slices` times the columns, rounded up to whole waves.
-__global__ __launch_bounds__(1024) void choose_join_kernel(const ChooseArgs a, int workgroups, int columns, int slices) {
-  extern __shared__ __attribute__((aligned(16))) char lds[];
-  const int E = a.E, e = threadIdx.x % columns, slice = threadIdx.x / columns;
-  float* sums = reinterpret_cast<float*>(lds);                              // [slices][E + 1]
-  int32_t* counts = reinterpret_cast<int32_t*>(sums + (size_t)slices * (E + 1));
-  float* waves = reinterpret_cast<float*>(counts + (size_t)slices * (E + 1));
-  if (e <= E && slice < slices) {
-    const int32_t* numbers = reinterpret_cast<const int32_t*>(a.work) + (size_t)workgroups * (E + 1);
-    float s = 0.f;
-    int32_t c = 0;
+// The workgroups' totals, summed in their order: a workgroup has 32 columns of them, eight
+// threads each.  The last one to be done, whichever it is, adds up what they made of the
+// balance loss, in their order.
+__global__ __launch_bounds__(256) void choose_join_kernel(const ChooseArgs a, int parts) {
+  __shared__ float sums[8][kJoinColumns];
+  __shared__ int32_t counts[8][kJoinColumns];
+  const int E = a.E, column = threadIdx.x % kJoinColumns, slice = threadIdx.x / kJoinColumns;
+  const int e = blockIdx.x * kJoinColumns + column;
+  const float* work = parts_of(a.work);
+  float s = 0.f;
+  int32_t c = 0;
+  if (e <= E) {
+    const int32_t* numbers = reinterpret_cast<const int32_t*>(work) + (size_t)parts * (E + 1);
 #pragma unroll 16
-    for (int w = slice; w < workgroups; w += slices) {
-      s += a.work[(size_t)w * (E + 1) + e];
+    for (int w = slice; w < parts; w += 8) {
+      s += work[(size_t)w * (E + 1) + e];
       c += numbers[(size_t)w * (E + 1) + e];
     }
-    sums[slice * (E + 1) + e] = s;
-    counts[slice * (E + 1) + e] = c;
   }
+  sums[slice][column] = s;
+  counts[slice][column] = c;
   __syncthreads();
+  if (threadIdx.x >= 64) return;
+  float part = 0.f;
   if (slice == 0 && e <= E) {
-    float s = 0.f;
-    int32_t c = 0;
-    for (int i = 0; i < slices; ++i) {
-      s += sums[i * (E + 1) + e];
-      c += counts[i * (E + 1) + e];
+    for (int i = 1; i < 8; ++i) {
+      s += sums[i][column];
+      c += counts[i][column];
     }
-    sums[e] = s;
-    counts[e] = c;
+    // At device scope: another workgroup reads the last column's.
+    __hip_atomic_store(&a.sums[e], s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __hip_atomic_store(&a.counts[e], c, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (e < E) part = (float)c * s;
   }
-  __syncthreads();
-  finish(a, sums, counts, waves);
+  part = sum_lanes(part, 64);
+  uint32_t done = 0;
+  if (threadIdx.x == 0) {
+    __hip_atomic_store(&a.work[1 + blockIdx.x], part, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");
+  if (threadIdx.x == 0)
+    done = __hip_atomic_fetch_add(reinterpret_cast<uint32_t*>(a.work), 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+  if (__builtin_amdgcn_readfirstlane(done) + 1 != gridDim.x) return;
+  if (threadIdx.x == 0) {
+    float all = 0.f;
+    for (unsigned i = 0; i < gridDim.x; ++i)
+      all += __hip_atomic_load(&a.work[1 + i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    const int32_t T = __hip_atomic_load(&a.counts[E], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    const float squares = __hip_atomic_load(&a.sums[E], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    const float per = T ? 1.f / (float)T : 0.f;
+    a.losses[0] = a.coef * all * per * per;
+    a.losses[1] = squares * per;
+  }
 }
 
 // With a_e = dlosses[0] E / (k T^2) counts[e], q = 2 dlosses[1] lse / T and p the
 // softmax: dlogits[e] = p_e (a_e - <p, a> + q), and of the weights w with gradients d,
 // in the chosen places w_j (d_j - <w, d>) where they are normalised, otherwise w_j d_j,
 // and -p_e <w, d> everywhere.  The softmax is found anew: its row is read anyway.
-template <int DT, int V>
+template <int V, int L>
 __global__ __launch_bounds__(256) void choose_backward_kernel(const ChooseArgs a) {
-  typedef Type<DT> T;
-  extern __shared__ __attribute__((aligned(16))) char lds[];
-  const Group g(a);
+  __shared__ float places[256 / L][V * L];  // of the chosen places, logit (u, lane, c) at ((u * 4 + c) * L + lane)
+  const int lane = threadIdx.x % L, own = threadIdx.x / L;
   const int E = a.E, k = a.k;
-  float* direct = reinterpret_cast<float*>(lds) + (size_t)g.own * a.lanes * V;  // of the chosen places, in the lanes' order
-  const int64_t n = (int64_t)blockIdx.x * g.groups + g.own;
+  float* direct = places[own];
+  const int64_t n = (int64_t)blockIdx.x * (256 / L) + own;
   const bool here = n < a.tokens;
   const bool live = here && (!a.live || a.live[n]);
   const char* row = a.logits + n * a.ld;
   float x[V];
-  if (live) {
-    load_logits<DT, V>(a, row, g.lane, x);
-  } else {
 #pragma unroll
-    for (int i = 0; i < V; ++i) x[i] = -__builtin_inff();
-  }
+  for (int i = 0; i < V; ++i) x[i] = -__builtin_inff();
+  if (live) load_logits<V, L>(a.dtype, E, row, lane, x);
 #pragma unroll
-  for (int i = 0; i < V; ++i) direct[i * a.lanes + g.lane] = 0.f;
-  const float top = top_of<V>(x, a.lanes);
+  for (int i = 0; i < V; ++i) direct[i * L + lane] = 0.f;
+  const float top = top_of<V, L>(x);
   const bool counted = top > -__builtin_inff();
-  const float sum = exponentials<V>(x, counted ? top : 0.f, a.lanes);
+  const float sum = exponentials<V, L>(x, counted ? top : 0.f);
   const float inv = counted ? 1.f / sum : 0.f;
   float shift = 0.f;  // of all places, times p
   float pull[V];
@@ -387,11 +488,11 @@ __global__ __launch_bounds__(256) void choose_backward_kernel(const ChooseArgs a
     float dot = 0.f;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      const int e = ((i / 4) * a.lanes + g.lane) * 4 + i % 4;
-      pull[i] = e < E ? scale * (float)a.counts[e] : 0.f;
+      const int e = (i / 4 * L + lane) * 4 + i % 4;
+      pull[i] = scale * (float)a.counts[e < E ? e : E - 1];
       dot = __builtin_fmaf(x[i] * inv, pull[i], dot);
     }
-    shift = 2.f * a.dlosses[1] * per * (top + logf(sum)) - sum_lanes(dot, a.lanes);
+    shift = 2.f * a.dlosses[1] * per * (top + logf(sum)) - sum_lanes(dot, L);
   } else {
 #pragma unroll
     for (int i = 0; i < V; ++i) pull[i] = 0.f;
@@ -404,31 +505,31 @@ __global__ __launch_bounds__(256) void choose_backward_kernel(const ChooseArgs a
     float from = top, over = sum;
     if (a.normalise) {
       from = -__builtin_inff();
-      for (int j = g.lane; j < k; j += a.lanes) {
+      for (int j = lane; j < k; j += L) {
         const int id = number(j);
-        if (id >= 0) from = fmaxf(from, logit_at<DT>(row, id));
+        if (id >= 0) from = fmaxf(from, logit_at(a, row, id));
       }
-      from = max_lanes(from, a.lanes);
+      from = max_lanes(from, L);
       over = 0.f;
-      for (int j = g.lane; j < k; j += a.lanes) {
+      for (int j = lane; j < k; j += L) {
         const int id = number(j);
-        if (id >= 0) over += __expf(logit_at<DT>(row, id) - from);
+        if (id >= 0) over += __expf(logit_at(a, row, id) - from);
       }
-      over = sum_lanes(over, a.lanes);
+      over = sum_lanes(over, L);
     }
     float dot = 0.f;
-    for (int j = g.lane; j < k; j += a.lanes) {
+    for (int j = lane; j < k; j += L) {
       const int id = number(j);
-      if (id >= 0) dot = __builtin_fmaf(__expf(logit_at<DT>(row, id) - from) / over, a.dweights[n * k + j], dot);
+      if (id >= 0) dot = __builtin_fmaf(__expf(logit_at(a, row, id) - from) / over, a.dweights[n * k + j], dot);
     }
-    dot = sum_lanes(dot, a.lanes);
+    dot = sum_lanes(dot, L);
     __builtin_amdgcn_wave_barrier();
-    for (int j = g.lane; j < k; j += a.lanes) {
+    for (int j = lane; j < k; j += L) {
       const int id = number(j);
       if (id < 0) continue;
-      const float w = __expf(logit_at<DT>(row, id) - from) / over;
-      const int quad = id >> 2;  // its place: number u * lanes + lane of the lanes' quads
-      const int at = ((quad >> a.lanes_shift) * 4 + (id & 3)) * a.lanes + (quad & (a.lanes - 1));
+      const float w = __expf(logit_at(a, row, id) - from) / over;
+      const int quad = id >> 2;
+      const int at = (quad / L * 4 + (id & 3)) * L + quad % L;
       atomicAdd(&direct[at], w * (a.dweights[n * k + j] - (a.normalise ? dot : 0.f)));
     }
     __builtin_amdgcn_wave_barrier();
@@ -438,55 +539,92 @@ __global__ __launch_bounds__(256) void choose_backward_kernel(const ChooseArgs a
   char* out = a.dlogits + n * a.ld_out;
 #pragma unroll
   for (int u = 0; u < V / 4; ++u) {
-    const int e = (u * a.lanes + g.lane) * 4;
+    const int e = (u * L + lane) * 4;
     float d[8] = {};
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
       const int i = 4 * u + c;
-      d[c] = counted ? __builtin_fmaf(x[i] * inv, pull[i] + shift, direct[i * a.lanes + g.lane]) : 0.f;
+      d[c] = counted ? __builtin_fmaf(x[i] * inv, pull[i] + shift, direct[i * L + lane]) : 0.f;
     }
-    if (e + 4 <= E) {
-      if constexpr (DT == 0) {
-        store16(out + e * 4, T::narrow(d));
+    if (a.dtype == EBAG_F32) {
+      if (e + 4 <= E) {
+        store16(out + e * 4, Type<0>::narrow(d));
       } else {
-        const vec16 v = T::narrow(d);
-        *reinterpret_cast<u32x2_any*>(out + e * 2) = u32x2_any{v[0], v[1]};
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          if (e + c < E) reinterpret_cast<float*>(out)[e + c] = d[c];
       }
     } else {
+      const vec16 v = a.dtype == EBAG_F16 ? Type<1>::narrow(d) : Type<2>::narrow(d);
+      if (e + 4 <= E) {
+        *reinterpret_cast<u32x2_any*>(out + e * 2) = u32x2_any{v[0], v[1]};
+      } else {
 #pragma unroll
-      for (int c = 0; c < 4; ++c)
-        if (e + c < E) reinterpret_cast<typename T::elt*>(out)[e + c] = T::narrow(d[c]);
+        for (int c = 0; c < 4; ++c)
+          if (e + c < E) reinterpret_cast<uint16_t*>(out)[e + c] = (uint16_t)(c & 1 ? v[c / 2] >> 16 : v[c / 2] & 0xffffu);
+      }
     }
   }
 }
 
 typedef void (*choose_fn)(const ChooseArgs);
 
-template <int DT>
-choose_fn pick_forward(int values, bool totals) {
-  if (totals) return values == 4 ? choose_kernel<DT, 4, true> : values == 8 ? choose_kernel<DT, 8, true> : choose_kernel<DT, 16, true>;
-  return values == 4 ? choose_kernel<DT, 4, false> : values == 8 ? choose_kernel<DT, 8, false> : choose_kernel<DT, 16, false>;
+// The instance for `lanes` lanes of `values` logits.
+template <bool TOTALS>
+choose_fn pick_forward(int values, int lanes, bool merge) {
+  if (values == 16) {
+    switch (lanes) {
+      case 4: return merge ? choose_kernel<16, 4, true, TOTALS> : choose_kernel<16, 4, false, TOTALS>;
+      case 8: return merge ? choose_kernel<16, 8, true, TOTALS> : choose_kernel<16, 8, false, TOTALS>;
+      case 16: return merge ? choose_kernel<16, 16, true, TOTALS> : choose_kernel<16, 16, false, TOTALS>;
+      default: return merge ? choose_kernel<16, 32, true, TOTALS> : choose_kernel<16, 32, false, TOTALS>;
+    }
+  }
+  if (values == 8) return choose_kernel<8, 64, false, TOTALS>;
+  switch (lanes) {
+    case 4: return choose_kernel<4, 4, false, TOTALS>;
+    case 8: return choose_kernel<4, 8, false, TOTALS>;
+    case 16: return choose_kernel<4, 16, false, TOTALS>;
+    case 32: return choose_kernel<4, 32, false, TOTALS>;
+    default: return choose_kernel<4, 64, false, TOTALS>;
+  }
 }
-template <int DT>
-choose_fn pick_backward(int values) {
-  return values == 4 ? choose_backward_kernel<DT, 4> : values == 8 ? choose_backward_kernel<DT, 8> : choose_backward_kernel<DT, 16>;
+choose_fn pick_backward(int values, int lanes) {
+  if (values == 16) {
+    switch (lanes) {
+      case 4: return choose_backward_kernel<16, 4>;
+      case 8: return choose_backward_kernel<16, 8>;
+      case 16: return choose_backward_kernel<16, 16>;
+      default: return choose_backward_kernel<16, 32>;
+    }
+  }
+  if (values == 8) return choose_backward_kernel<8, 64>;
+  switch (lanes) {
+    case 4: return choose_backward_kernel<4, 4>;
+    case 8: return choose_backward_kernel<4, 8>;
+    case 16: return choose_backward_kernel<4, 16>;
+    case 32: return choose_backward_kernel<4, 32>;
+    default: return choose_backward_kernel<4, 64>;
+  }
 }
 
 int hipf(hipError_t e, const char* what) { return fail(EBAG_EHIP, "%s: %s", what, hipGetErrorString(e)); }
 
-// Logits of a lane: few where there are few tokens, so that their steps are short and spread over the card; many
-// where the card is full anyway.
-int values_for(int64_t tokens, int E) {
-  for (int v = 16; v > 4; v /= 2) {
-    int lanes = kLeastLanes;
-    while (lanes * v < E) lanes *= 2;
-    if (tokens * lanes >= 64 * 2048) return v;
+// Lanes of a token and logits of a lane.  Four logits where there are few tokens, so that the steps are short and
+// spread over the card; 16, with fewer steps over the lanes, where the card is full with them.
+void shape_for(int64_t tokens, int E, int* values, int* lanes) {
+  *lanes = 4;
+  if (E > 32) {
+    while (*lanes * 16 < E) *lanes *= 2;
+    *values = 16;
+    if (tokens * *lanes >= 64 * 2048) return;
   }
-  return E > 256 ? 8 : 4;
+  *values = E > 256 ? 8 : 4;
+  while (*lanes * *values < E) *lanes *= 2;
 }
 
 int choose_args(ebag_a2a_moe_t h, const void* logits, int64_t ldl, int32_t dtype, int64_t tokens, const uint8_t* live,
-                int32_t normalise, ChooseArgs* a, int* values) {
+                int32_t normalise, ChooseArgs* a, int* values, int* lanes) {
   if (int rc = check_moe_plan(h, tokens)) return rc;
   if (dtype != EBAG_F32 && dtype != EBAG_F16 && dtype != EBAG_BF16) return fail(EBAG_EINVAL, "bad dtype %d", (int)dtype);
   if (normalise != 0 && normalise != 1) return fail(EBAG_EINVAL, "normalise must be 0 or 1");
@@ -504,16 +642,11 @@ int choose_args(ebag_a2a_moe_t h, const void* logits, int64_t ldl, int32_t dtype
   a->tokens = tokens;
   a->E = h->experts;
   a->k = h->choices;
+  a->dtype = dtype;
   a->normalise = normalise;
   a->coef = (float)((double)h->experts / h->choices);
   a->turns = 1;
-  *values = values_for(tokens, a->E);
-  a->lanes = kLeastLanes;
-  a->lanes_shift = 2;
-  while (a->lanes * *values < a->E) {
-    a->lanes *= 2;
-    ++a->lanes_shift;
-  }
+  shape_for(tokens, a->E, values, lanes);
   return EBAG_OK;
 }
 
@@ -522,15 +655,15 @@ int choose_args(ebag_a2a_moe_t h, const void* logits, int64_t ldl, int32_t dtype
 extern "C" {
 
 int64_t ebag_a2a_moe_choose_work(ebag_a2a_moe_t h) {
-  return h ? (int64_t)kMostParts * 2 * (h->experts + 1) : 0;
+  return h ? 32 + (int64_t)kMostParts * 2 * (h->experts + 1) : 0;
 }
 
 int ebag_a2a_moe_choose(ebag_a2a_moe_t h, const void* logits, int64_t ldl, int32_t dtype, int64_t tokens,
                         const float* bias, const uint8_t* live, int32_t normalise, int32_t* ids, float* weights,
                         int32_t* counts, float* sums, float* losses, float* work, hipStream_t stream) {
   ChooseArgs a;
-  int values;
-  if (int rc = choose_args(h, logits, ldl, dtype, tokens, live, normalise, &a, &values)) return rc;
+  int values, lanes;
+  if (int rc = choose_args(h, logits, ldl, dtype, tokens, live, normalise, &a, &values, &lanes)) return rc;
   if (tokens && (!ids || !weights)) return fail(EBAG_EINVAL, "null ids or weights");
   const bool totals = counts || sums || losses || work;
   if (totals && (!counts || !sums || !losses || !work))
@@ -545,9 +678,9 @@ int ebag_a2a_moe_choose(ebag_a2a_moe_t h, const void* logits, int64_t ldl, int32
   a.work = work;
   // With totals large workgroups, as every one of them leaves a part to be joined.
   int threads = 256;
-  if (totals && tokens * a.lanes > 256 * 64) threads = 1024;
-  while (threads > 256 && threads / a.lanes * a.k > 6144) threads /= 2;  // 48 KiB of choices
-  const int groups = threads / a.lanes;
+  if (totals && tokens * lanes > 256 * 64) threads = 1024;
+  while (threads > 256 && threads / lanes * a.k > 6144) threads /= 2;  // 48 KiB of choices
+  const int groups = threads / lanes;
   int64_t wgs = (tokens + groups - 1) / groups;
   if (wgs < 1) wgs = 1;
   if (totals && wgs > kMostParts) {
@@ -557,16 +690,13 @@ int ebag_a2a_moe_choose(ebag_a2a_moe_t h, const void* logits, int64_t ldl, int32
   if (wgs > INT_MAX) return fail(EBAG_EINVAL, "too many tokens for one launch");
   size_t lds = (size_t)groups * a.k * 8;
   if (totals) lds += (size_t)(a.E + 1) * 4 * (1 + threads / 64) + 64;
-  const choose_fn fn = dtype == EBAG_F32   ? pick_forward<0>(values, totals)
-                       : dtype == EBAG_F16 ? pick_forward<1>(values, totals)
-                                           : pick_forward<2>(values, totals);
+  const bool merge = a.k > 2 && a.k <= 8;
+  const choose_fn fn = totals ? pick_forward<true>(values, lanes, merge) : pick_forward<false>(values, lanes, merge);
   hipLaunchKernelGGL(fn, dim3((unsigned)wgs), dim3(threads), lds, stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return hipf(e, "launch the choice");
   if (!totals || wgs == 1) return EBAG_OK;
-  const int columns = (a.E + 1 + 63) / 64 * 64, slices = 1024 / columns;
-  hipLaunchKernelGGL(choose_join_kernel, dim3(1), dim3(columns * slices), (size_t)slices * (a.E + 1) * 8 + 64, stream, a,
-                     (int)wgs, columns, slices);
+  hipLaunchKernelGGL(choose_join_kernel, dim3(a.E / kJoinColumns + 1), dim3(256), 0, stream, a, (int)wgs);
   e = hipGetLastError();
   return e == hipSuccess ? EBAG_OK : hipf(e, "launch the choice's totals");
 }
@@ -576,8 +706,8 @@ int ebag_a2a_moe_choose_backward(ebag_a2a_moe_t h, const void* logits, int64_t l
                                  const int32_t* counts, const float* dlosses, void* dlogits, int64_t lddl,
                                  hipStream_t stream) {
   ChooseArgs a;
-  int values;
-  if (int rc = choose_args(h, logits, ldl, dtype, tokens, live, normalise, &a, &values)) return rc;
+  int values, lanes;
+  if (int rc = choose_args(h, logits, ldl, dtype, tokens, live, normalise, &a, &values, &lanes)) return rc;
   if (!tokens) return EBAG_OK;
   if (!dlogits) return fail(EBAG_EINVAL, "null dlogits");
   if (dweights && !ids) return fail(EBAG_EINVAL, "null ids");
@@ -592,13 +722,10 @@ int ebag_a2a_moe_choose_backward(ebag_a2a_moe_t h, const void* logits, int64_t l
   a.dlosses = dlosses;
   a.dlogits = static_cast<char*>(dlogits);
   a.ld_out = lddl * elt;
-  const int groups = 256 / a.lanes;
+  const int groups = 256 / lanes;
   const int64_t wgs = (tokens + groups - 1) / groups;
   if (wgs > INT_MAX) return fail(EBAG_EINVAL, "too many tokens for one launch");
-  const choose_fn fn = dtype == EBAG_F32   ? pick_backward<0>(values)
-                       : dtype == EBAG_F16 ? pick_backward<1>(values)
-                                           : pick_backward<2>(values);
-  hipLaunchKernelGGL(fn, dim3((unsigned)wgs), dim3(256), (size_t)256 * values * 4, stream, a);
+  hipLaunchKernelGGL(pick_backward(values, lanes), dim3((unsigned)wgs), dim3(256), 0, stream, a);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? EBAG_OK : hipf(e, "launch the choice's gradient");
 }

@@ -47,7 +47,7 @@ def _args(**kw):
     import torch
     i32 = dict(dtype=torch.int32)
     a = dict(logits=torch.zeros(3, 4), ids=torch.zeros(3, 2, **i32), weights=torch.zeros(3, 2), counts=torch.zeros(5, **i32),
-             sums=torch.zeros(5), losses=torch.zeros(2), work=torch.zeros(512 * 5), bias=torch.zeros(4),
+             sums=torch.zeros(5), losses=torch.zeros(2), work=torch.zeros(32 + 512 * 5), bias=torch.zeros(4),
              live=torch.zeros(3, dtype=torch.bool))
     a.update(kw)
     return {n: None if t is None else _On(t) for n, t in a.items()}
