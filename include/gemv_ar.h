@@ -201,6 +201,70 @@ int gemv_ar_q4_experts(gemv_ar_q4_t h, const uint8_t* codes, const void* scales,
 /* Release the plan.  NULL is ignored. */
 void gemv_ar_q4_destroy(gemv_ar_q4_t h);
 
+/*
+ * Products in 8-bit integers, with a scale for each token and for each channel.
+ *
+ * E matrices of M x K weights (E = experts; 1 for a plain layer) in 8 bits:
+ *
+ *   W[e][m][k] = scales[e][m] * codes[e][m][k]
+ *
+ *   codes   int8 [E][M][pitch], pitch = K rounded up to a multiple of 128
+ *           (gemv_ar_q8_pitch); columns from K on may hold anything
+ *   scales  fp32 [E][M]
+ *
+ * Rows of x (of the plan's type dtype) are rounded to 8 bits themselves, each with
+ * a scale of its own: xs[n] = max_k |x[n][k]| / 127, rounded to fp32, and xq[n][k] the
+ * whole number nearest to x[n][k] / xs[n] (halves to even, kept in -127 .. 127).  A
+ * row of zeros has the scale 0; a row with an infinity or NaN the scale NaN and codes
+ * of 0, and so NaN in its own row of y and no other.
+ *
+ *   xq  int8 [rows][pitch], zeros from column K on        xs  fp32 [rows]
+ *
+ *   forward: y[n][m] = xs[n] scales[0][m] sum_k xq[n][k] codes[0][m][k],   n < rows
+ *   experts: the same of row p with expert e's matrix,   offsets[e] <= p < offsets[e + 1]
+ *
+ * With glu = 1 the M rows are M / 2 gate rows and M / 2 up rows and the result
+ * has M / 2 columns, y = silu(gate) * up, silu(v) = v / (1 + exp(-v)).
+ *
+ * The sums are whole numbers and exact (K at most 2^17); each is rounded to fp32,
+ * times the product of its scales, and once to y's type, the plan's or fp32.  Row r
+ * of x starts at element r * ldx, of y at element r * ldy; neither needs an alignment
+ * beyond its elements'; codes and xq are 16-byte aligned.  Outputs must not overlap inputs.
+ * Results do not depend on the other rows' values and are the same bits on every run.
+ */
+typedef struct gemv_ar_q8_plan* gemv_ar_q8_t;
+
+/* Create a plan on the current HIP device for E = experts (1..512) matrices of M
+ * rows (below 2^31) and K columns (1..2^17), glu 0 or 1 (M even).  It owns no device
+ * memory; its calls share nothing but the xq and xs that the caller gives to several,
+ * may run on any stream and can be captured into a graph.  They must be made with the
+ * plan's device current (EBAG_EINVAL otherwise). */
+int gemv_ar_q8_create(gemv_ar_q8_t* out, int64_t M, int64_t K, int32_t dtype, int32_t experts, int32_t glu);
+
+/* Bytes of a row of codes and of xq. */
+int64_t gemv_ar_q8_pitch(gemv_ar_q8_t h);
+
+/* Round weights w [E][M][K] (contiguous, of dtype) to 8 bits, a row as a row of x is. */
+int gemv_ar_q8_quantize(gemv_ar_q8_t h, const void* w, int8_t* codes, float* scales, hipStream_t stream);
+
+/* Round rows x [rows][K] to xq and xs, for several products of the same rows. */
+int gemv_ar_q8_round(gemv_ar_q8_t h, const void* x, int64_t ldx, int64_t rows, int8_t* xq, float* xs, hipStream_t stream);
+
+/* x [rows][K] times the (first) matrix: y [rows][M, or M / 2 with glu].  xq and xs are
+ * the call's scratch memory and hold nothing of use behind it; with x NULL they are the
+ * rows, as gemv_ar_q8_round left them. */
+int gemv_ar_q8_forward(gemv_ar_q8_t h, const int8_t* codes, const float* scales, const void* x, int64_t ldx, int64_t rows,
+                       int8_t* xq, float* xs, void* y, int64_t ldy, int32_t y_dtype, hipStream_t stream);
+
+/* Every expert's rows times its matrix.  offsets, src, choices, x_rows and rows as for
+ * gemv_ar_q4_experts; x, xq and xs as for gemv_ar_q8_forward, with x_rows rows. */
+int gemv_ar_q8_experts(gemv_ar_q8_t h, const int8_t* codes, const float* scales, const void* x, int64_t ldx, int64_t x_rows,
+                       int8_t* xq, float* xs, const int32_t* offsets, const int32_t* src, int32_t choices, int64_t rows,
+                       void* y, int64_t ldy, int32_t y_dtype, hipStream_t stream);
+
+/* Release the plan.  NULL is ignored. */
+void gemv_ar_q8_destroy(gemv_ar_q8_t h);
+
 #ifdef __cplusplus
 }
 #endif

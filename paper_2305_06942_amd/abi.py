@@ -117,6 +117,15 @@ _SIGS = {
     "gemv_ar_q4_experts": ([_P, _P, _P, _P, _P, ctypes.c_int64, ctypes.c_int64, _P, _P, ctypes.c_int32, ctypes.c_int64,
                             _P, ctypes.c_int64, ctypes.c_int32, _P], ctypes.c_int),
     "gemv_ar_q4_destroy": ([_P], None),
+    "gemv_ar_q8_create": ([_P, ctypes.c_int64, ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32], ctypes.c_int),
+    "gemv_ar_q8_pitch": ([_P], ctypes.c_int64),
+    "gemv_ar_q8_quantize": ([_P, _P, _P, _P, _P], ctypes.c_int),
+    "gemv_ar_q8_round": ([_P, _P, ctypes.c_int64, ctypes.c_int64, _P, _P, _P], ctypes.c_int),
+    "gemv_ar_q8_forward": ([_P, _P, _P, _P, ctypes.c_int64, ctypes.c_int64, _P, _P, _P, ctypes.c_int64, ctypes.c_int32, _P],
+                           ctypes.c_int),
+    "gemv_ar_q8_experts": ([_P, _P, _P, _P, ctypes.c_int64, ctypes.c_int64, _P, _P, _P, _P, ctypes.c_int32, ctypes.c_int64,
+                            _P, ctypes.c_int64, ctypes.c_int32, _P], ctypes.c_int),
+    "gemv_ar_q8_destroy": ([_P], None),
 }
 
 
@@ -765,6 +774,94 @@ class Q4Gemv:
     def close(self):
         if getattr(self, "_h", None):
             self._lib.gemv_ar_q4_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class Q8Gemv:
+    """A plan for products in 8-bit integers with a scale for each token and each
+    channel (``gemv_ar_q8_create``): `experts` matrices of M rows and K columns,
+    x of dtype; glu=1: y = silu(gate) * up of the two halves of the M rows.
+    Methods mirror the C ABI and take torch tensors: codes int8 [experts, M,
+    pitch], scales float32 [experts, M], xq int8 [rows, pitch] and xs float32
+    [rows], x and y with any step between rows, y of the plan's type or float32."""
+
+    def __init__(self, M: int, K: int, dtype: int, experts: int = 1, glu: int = 0):
+        lib = load()
+        h = ctypes.c_void_p()
+        _check(lib.gemv_ar_q8_create(ctypes.byref(h), int(M), int(K), int(dtype), int(experts), int(glu)))
+        self._h = h
+        self._lib = lib
+        self._shape(M, K, dtype, experts, glu)
+
+    def _shape(self, M, K, dtype, experts, glu):
+        self.M, self.K, self.matrices = int(M), int(K), int(experts)
+        self.pitch = -(-self.K // 128) * 128  # gemv_ar_q8_pitch
+        self.wide = self.M // 2 if glu else self.M
+        self.kind = {v: n for n, v in ROW_TYPES.items()}[int(dtype)]
+        import torch
+        self._i8, self._i32, self._f32, self._dtype = torch.int8, torch.int32, torch.float32, getattr(torch, self.kind)
+        self._rows = self.matrices * self.M
+
+    def _weights(self, codes, scales):
+        if not (_fit(codes, self._i8, self._rows * self.pitch) and _fit(scales, self._f32, self._rows)):
+            _refuse((codes, "codes", ("int8",), self._rows * self.pitch), (scales, "scales", F32, 4 * self._rows))
+
+    def _x(self, x, xq, xs, rows):
+        """(address, row step) of x, or of none; checks the rows' memory in 8 bits."""
+        if not (_fit(xq, self._i8, rows * self.pitch) and _fit(xs, self._f32, rows)):
+            _refuse((xq, "xq", ("int8",), rows * self.pitch), (xs, "xs", F32, 4 * rows))
+        if x is None:
+            return None, self.K
+        px, ldx, _ = _matrix(x, rows, self.K, self.kind, "x")
+        return px, ldx
+
+    def _y(self, y, rows):
+        kind = self.kind if y.dtype is self._dtype or y.dtype is not self._f32 else "float32"
+        py, ldy, _ = _matrix(y, rows, self.wide, kind, "y")
+        return py, ldy, ROW_TYPES[kind]
+
+    def quantize(self, w, codes, scales, stream=None):
+        self._weights(codes, scales)
+        if not _fit(w, self._dtype, self._rows * self.K):
+            _refuse((w, "w", (self.kind,), self._rows * self.K * self._dtype.itemsize))
+        _check(self._lib.gemv_ar_q8_quantize(self._h, w.data_ptr(), codes.data_ptr(), scales.data_ptr(), _stream(stream)))
+
+    def round(self, x, xq, xs, stream=None):
+        rows = x.shape[0]
+        px, ldx = self._x(x, xq, xs, rows)
+        _check(self._lib.gemv_ar_q8_round(self._h, px, ldx, rows, xq.data_ptr(), xs.data_ptr(), _stream(stream)))
+
+    def forward(self, codes, scales, x, y, xq, xs, stream=None):
+        """gemv_ar_q8_forward; x None: the rows are those that round() left in xq and xs, as many as y has."""
+        self._weights(codes, scales)
+        rows = y.shape[0] if x is None else x.shape[0]
+        px, ldx = self._x(x, xq, xs, rows)
+        py, ldy, y_type = self._y(y, rows)
+        _check(self._lib.gemv_ar_q8_forward(self._h, codes.data_ptr(), scales.data_ptr(), px, ldx, rows, xq.data_ptr(),
+                                            xs.data_ptr(), py, ldy, y_type, _stream(stream)))
+
+    def experts(self, codes, scales, x, offsets, y, xq, xs, src=None, k=1, stream=None):
+        """gemv_ar_q8_experts; k: choices of a token, which src counts in; x None: the rows are xq's and xs's."""
+        self._weights(codes, scales)
+        if not (_fit(offsets, self._i32, self.matrices + 1) and (src is None or _fit(src, self._i32, 0))):
+            _refuse((offsets, "offsets", I32, 4 * (self.matrices + 1)), (src, "src", I32, 0))
+        x_rows = xs.numel() if x is None else x.shape[0]
+        rows = x_rows if src is None else src.numel()
+        px, ldx = self._x(x, xq, xs, x_rows)
+        py, ldy, y_type = self._y(y, rows)
+        _check(self._lib.gemv_ar_q8_experts(self._h, codes.data_ptr(), scales.data_ptr(), px, ldx, x_rows, xq.data_ptr(),
+                                            xs.data_ptr(), offsets.data_ptr(), _addr(src), int(k), rows, py, ldy, y_type,
+                                            _stream(stream)))
+
+    def close(self):
+        if getattr(self, "_h", None):
+            self._lib.gemv_ar_q8_destroy(self._h)
             self._h = None
 
     def __del__(self):

@@ -1,0 +1,348 @@
+// Products in 8-bit integers (gemv_ar_q8_* of include/gemv_ar.h): rounding to 8
+// bits, and the host side: checks, launch shapes, the choice of kernel.
+#include <hip/hip_runtime.h>
+
+#include <climits>
+#include <new>
+
+#include "ebag_a2a.h"
+#include "gemv_ar.h"
+#include "q8.h"
+
+using namespace ebag;
+
+namespace {
+
+// ------------------------------------------------------------------- to 8 bits
+
+constexpr int kRoundThreads = 256;
+constexpr int kHeld = 4;  // units of 8 elements that a lane holds
+
+struct RoundArgs {
+  const char* x;
+  int8_t* codes;
+  float* scales;
+  int64_t ld;       // bytes
+  int64_t pitch;
+  int64_t rows;
+  int32_t K;
+  int32_t units;    // of 8 elements, the last one short or empty: pitch / 8
+};
+
+// The largest over the 64 lanes, in each of them; of numbers without a sign, as whole numbers keep the order of
+// floats and put NaN above infinity.
+__device__ __forceinline__ uint32_t largest(uint32_t v) {
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const uint32_t o = __shfl_xor(v, d);
+    v = v > o ? v : o;
+  }
+  return v;
+}
+
+// Eight neighbouring elements in fp32, zeros behind the row's end.
+template <int DT>
+__device__ __forceinline__ void load8(const char* row, int at, int K, float* f) {
+  typedef Type<DT> T;
+  typedef typename T::elt elt;
+  if (at + 8 <= K) {
+#pragma unroll
+    for (int v = 0; v < 8 / T::N; ++v) T::widen(load16(row + (int64_t)at * sizeof(elt) + 16 * v), f + v * T::N);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = at + i < K ? T::widen(reinterpret_cast<const elt*>(row)[at + i]) : 0.f;
+  }
+}
+
+// The whole number nearest to x / scale, halves to even: what the product with the reciprocal gives is at most one
+// off, and x less that many scales, exact up to its sign and its order with scale / 2, says which way.
+struct Rounder {
+  float scale, inv, half, factor;
+  bool any;
+  __device__ __forceinline__ Rounder(float s) {
+    // Scales so small that their reciprocal would not be a number, or their half not exact, are taken 2^64 times.
+    factor = s < 0x1p-60f ? 0x1p64f : 1.f;
+    scale = s * factor;
+    any = s > 0.f;  // not NaN
+    inv = any ? 1.f / scale : 0.f;
+    half = 0.5f * scale;
+  }
+  __device__ __forceinline__ int code(float x) const {
+    x *= factor;
+    float q = rintf(x * inv);
+    const float left = fmaf(-q, scale, x), size = fabsf(left);
+    if (size > half || (size == half && ((int)q & 1))) q += left > 0.f ? 1.f : -1.f;
+    return any ? (int)fminf(fmaxf(q, -127.f), 127.f) : 0;
+  }
+};
+
+__device__ __forceinline__ void store8(int8_t* to, const Rounder& r, const float* f) {
+  uint32_t w[2] = {0, 0};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) w[i / 4] |= ((uint32_t)r.code(f[i]) & 0xffu) << (8 * (i % 4));
+  *reinterpret_cast<uint2*>(to) = uint2{w[0], w[1]};
+}
+
+// WAVE: a wave to a row, otherwise a workgroup.  Up to 32 elements of a lane stay in registers between
+// the largest and the codes; longer rows are read again.
+template <int DT, bool WAVE>
+__global__ __launch_bounds__(kRoundThreads) void q8_round_kernel(const RoundArgs a) {
+  __shared__ uint32_t tops[kRoundThreads / 64];
+  const int lanes = WAVE ? 64 : kRoundThreads, lane = threadIdx.x % lanes;
+  const int64_t row = WAVE ? (int64_t)blockIdx.x * (kRoundThreads / 64) + threadIdx.x / 64 : blockIdx.x;
+  if (WAVE && row >= a.rows) return;
+  const char* x = a.x + row * a.ld;
+  int8_t* codes = a.codes + row * a.pitch;
+  float held[kHeld][8];
+  uint32_t top = 0;
+  auto look = [&](const float* f) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t v = __float_as_uint(f[i]) & 0x7fffffffu;
+      top = top > v ? top : v;
+    }
+  };
+#pragma unroll
+  for (int u = 0; u < kHeld; ++u) {
+    const int unit = u * lanes + lane;
+    if (unit < a.units) {
+      load8<DT>(x, unit * 8, a.K, held[u]);
+      look(held[u]);
+    }
+  }
+  for (int unit = kHeld * lanes + lane; unit < a.units; unit += lanes) {
+    float f[8];
+    load8<DT>(x, unit * 8, a.K, f);
+    look(f);
+  }
+  top = largest(top);
+  if (!WAVE) {
+    if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kRoundThreads / 64; ++w) top = top > tops[w] ? top : tops[w];
+  }
+  const float scale = top >= 0x7f800000u ? __builtin_nanf("") : __uint_as_float(top) / 127.f;
+  if (lane == 0) a.scales[row] = scale;
+  const Rounder r(scale);
+#pragma unroll
+  for (int u = 0; u < kHeld; ++u) {
+    const int unit = u * lanes + lane;
+    if (unit < a.units) store8(codes + unit * 8, r, held[u]);
+  }
+  for (int unit = kHeld * lanes + lane; unit < a.units; unit += lanes) {
+    float f[8];
+    load8<DT>(x, unit * 8, a.K, f);
+    store8(codes + unit * 8, r, f);
+  }
+}
+
+int hipf(hipError_t e, const char* what) { return fail(EBAG_EHIP, "%s: %s", what, hipGetErrorString(e)); }
+
+}  // namespace
+
+struct gemv_ar_q8_plan {
+  int device = 0;
+  int64_t M = 0, K = 0, pitch = 0;
+  int32_t dtype = 0, experts = 0, glu = 0;
+};
+
+namespace {
+
+int check_plan(const gemv_ar_q8_plan* h) {
+  if (!h) return fail(EBAG_EINVAL, "null plan");
+  int dev = -1;
+  if (hipGetDevice(&dev) != hipSuccess || dev != h->device)
+    return fail(EBAG_EINVAL, "the plan belongs to device %d, but device %d is current", h->device, dev);
+  return EBAG_OK;
+}
+
+int elt_of(int dtype) { return dtype == EBAG_F32 ? 4 : 2; }
+
+int check_x(const gemv_ar_q8_plan* h, const void* x, int64_t ldx, const int8_t* xq, const float* xs) {
+  if (!xq || !xs) return fail(EBAG_EINVAL, "null xq or xs");
+  if (reinterpret_cast<uintptr_t>(xq) % 16 || reinterpret_cast<uintptr_t>(xs) % 4)
+    return fail(EBAG_EINVAL, "xq not aligned to 16 bytes or xs not to its elements");
+  if (!x) return EBAG_OK;
+  if (reinterpret_cast<uintptr_t>(x) % elt_of(h->dtype)) return fail(EBAG_EINVAL, "x not aligned to its elements");
+  if (ldx < h->K || ldx > (int64_t)1 << 40) return fail(EBAG_EINVAL, "row step %lld of x below K=%lld", (long long)ldx, (long long)h->K);
+  return EBAG_OK;
+}
+
+int launch_round(const gemv_ar_q8_plan* h, const void* x, int64_t ldx, int64_t rows, int8_t* xq, float* xs, hipStream_t stream) {
+  RoundArgs a{};
+  a.x = static_cast<const char*>(x);
+  a.codes = xq;
+  a.scales = xs;
+  a.ld = ldx * elt_of(h->dtype);
+  a.pitch = h->pitch;
+  a.rows = rows;
+  a.K = (int32_t)h->K;
+  a.units = (int32_t)(h->pitch / 8);
+  const bool wave = h->K <= 64 * 8 * kHeld;
+  const int64_t per_wg = wave ? kRoundThreads / 64 : 1, wgs = (rows + per_wg - 1) / per_wg;
+  if (wgs > INT_MAX) return fail(EBAG_EUNSUPPORTED, "too many rows for one launch");
+  void (*fn)(const RoundArgs) = h->dtype == EBAG_F32   ? wave ? q8_round_kernel<0, true> : q8_round_kernel<0, false>
+                                : h->dtype == EBAG_F16 ? wave ? q8_round_kernel<1, true> : q8_round_kernel<1, false>
+                                : wave                 ? q8_round_kernel<2, true>
+                                                       : q8_round_kernel<2, false>;
+  hipLaunchKernelGGL(fn, dim3((unsigned)wgs), dim3(kRoundThreads), 0, stream, a);
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? EBAG_OK : hipf(e, "launch the rounding to 8 bits");
+}
+
+int fill_args(const gemv_ar_q8_plan* h, const int8_t* codes, const float* scales, const void* x, int64_t ldx, int64_t x_rows,
+              const int8_t* xq, const float* xs, int64_t rows, void* y, int64_t ldy, int32_t y_dtype, Q8Args* a) {
+  if (y_dtype != h->dtype && y_dtype != EBAG_F32)
+    return fail(EBAG_EINVAL, "y_dtype must be fp32 or the plan's type, not %d", (int)y_dtype);
+  if (!codes || !scales || !y) return fail(EBAG_EINVAL, "null codes, scales or y");
+  if (int rc = check_x(h, x, ldx, xq, xs)) return rc;
+  const int y_elt = elt_of(y_dtype);
+  const int64_t wide = h->glu ? h->M / 2 : h->M;
+  if (reinterpret_cast<uintptr_t>(codes) % 16) return fail(EBAG_EINVAL, "codes not aligned to 16 bytes");
+  if (reinterpret_cast<uintptr_t>(scales) % 4 || reinterpret_cast<uintptr_t>(y) % y_elt)
+    return fail(EBAG_EINVAL, "scales or y not aligned to its elements");
+  if (ldy < wide || ldy > (int64_t)1 << 40) return fail(EBAG_EINVAL, "row step %lld of y below its %lld columns", (long long)ldy, (long long)wide);
+  *a = Q8Args{};
+  a->codes = codes;
+  a->scales = scales;
+  a->xq = xq;
+  a->xs = xs;
+  a->y = static_cast<char*>(y);
+  a->ldy = ldy * y_elt;
+  a->pitch = h->pitch;
+  a->M = h->M;
+  a->out_rows = wide;
+  a->x_rows = x_rows;
+  a->rows = (uint32_t)rows;
+  a->experts = h->experts;
+  a->glu = h->glu;
+  a->y_type = y_dtype;
+  a->by_choices = make_divisor(1);
+  return EBAG_OK;
+}
+
+int launch_few(Q8Args a, int x_tiles, hipStream_t stream) {
+  const int cols = 16 * x_tiles;
+  const int64_t slots = a.offsets ? most_tiles(a.rows, a.experts, cols) : (a.rows + cols - 1) / cols;
+  const int64_t singles = (a.out_rows + 15) / 16 * slots;  // tiles of 16 columns of y
+  const int tiles = a.glu || singles >= 4096 ? 2 : 1;
+  const int64_t wave_cols = a.glu ? 16 : 16 * tiles;
+  const int64_t all_tiles = (a.out_rows + wave_cols - 1) / wave_cols * slots, lines = a.pitch / kQ8Line;
+  a.split = 1;
+  while (a.split < 8 && all_tiles * a.split < 4096 && lines >= 4 * a.split) a.split *= 2;
+  const int waves = a.split > 4 ? 8 : 4;
+  const int64_t wg_cols = wave_cols * (waves / a.split), grid_tiles = (a.out_rows + wg_cols - 1) / wg_cols;
+  if (grid_tiles * slots > INT_MAX) return fail(EBAG_EUNSUPPORTED, "too many tiles for one launch");
+  a.by_tiles = make_divisor(grid_tiles);
+  launch_q8_few(a, tiles, x_tiles, (unsigned)(grid_tiles * slots), 64 * waves, stream);
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? EBAG_OK : hipf(e, "launch the product in 8 bits");
+}
+
+int launch_tile(Q8Args a, int x_rows, hipStream_t stream) {
+  const int64_t per_wg = kQ8TileRows / (a.glu ? 2 : 1), tiles = (a.out_rows + per_wg - 1) / per_wg;
+  const int64_t slots = a.offsets ? most_tiles(a.rows, a.experts, x_rows) : (a.rows + x_rows - 1) / x_rows;
+  const int64_t grid = (slots + 3) / 4 * 4 * tiles;
+  if (grid > INT_MAX) return fail(EBAG_EUNSUPPORTED, "too many tiles for one launch");
+  a.by_tiles = make_divisor(tiles);
+  a.whole = (uint32_t)(grid / 256 * 256);
+  launch_q8_tile(a, x_rows, (unsigned)grid, stream);
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? EBAG_OK : hipf(e, "launch the product in 8 bits");
+}
+
+int launch(const Q8Args& a, hipStream_t stream) {
+  const double each = a.offsets ? (double)a.rows / a.experts : a.rows;  // rows of a matrix
+  if (each <= 16) return launch_few(a, 1, stream);
+  if (each <= 32) return launch_few(a, 2, stream);
+  if (each <= 64) return launch_few(a, 4, stream);
+  return launch_tile(a, each <= 128 ? 64 : each <= 1024 ? 128 : 256, stream);
+}
+
+}  // namespace
+
+extern "C" {
+
+int gemv_ar_q8_create(gemv_ar_q8_t* out, int64_t M, int64_t K, int32_t dtype, int32_t experts, int32_t glu) {
+  if (!out) return fail(EBAG_EINVAL, "null output handle");
+  *out = nullptr;
+  if (M < 1 || M > INT_MAX) return fail(EBAG_EINVAL, "M=%lld outside [1, 2^31)", (long long)M);
+  if (K < 1 || K > 1 << 17) return fail(EBAG_EINVAL, "K=%lld outside [1, 2^17]", (long long)K);
+  if (dtype != EBAG_F32 && dtype != EBAG_F16 && dtype != EBAG_BF16) return fail(EBAG_EINVAL, "bad dtype %d", (int)dtype);
+  if (experts < 1 || experts > 512) return fail(EBAG_EINVAL, "experts=%d outside [1, 512]", experts);
+  if (glu != 0 && glu != 1) return fail(EBAG_EINVAL, "glu must be 0 or 1");
+  if (glu && M % 2) return fail(EBAG_EINVAL, "glu needs an even M, not %lld", (long long)M);
+  gemv_ar_q8_plan* h = new (std::nothrow) gemv_ar_q8_plan();
+  if (!h) return fail(EBAG_ENOMEM, "host allocation failed");
+  const hipError_t e = hipGetDevice(&h->device);
+  if (e != hipSuccess) {
+    delete h;
+    return hipf(e, "query device");
+  }
+  h->M = M;
+  h->K = K;
+  h->pitch = q8_pitch(K);
+  h->dtype = dtype;
+  h->experts = experts;
+  h->glu = glu;
+  *out = h;
+  clear_error();
+  return EBAG_OK;
+}
+
+int64_t gemv_ar_q8_pitch(gemv_ar_q8_t h) { return h ? h->pitch : 0; }
+
+int gemv_ar_q8_quantize(gemv_ar_q8_t h, const void* w, int8_t* codes, float* scales, hipStream_t stream) {
+  if (int rc = check_plan(h)) return rc;
+  if (!w || !codes || !scales) return fail(EBAG_EINVAL, "null w, codes or scales");
+  if (reinterpret_cast<uintptr_t>(codes) % 16) return fail(EBAG_EINVAL, "codes not aligned to 16 bytes");
+  if (reinterpret_cast<uintptr_t>(w) % elt_of(h->dtype) || reinterpret_cast<uintptr_t>(scales) % 4)
+    return fail(EBAG_EINVAL, "w or scales not aligned to its elements");
+  return launch_round(h, w, h->K, h->M * h->experts, codes, scales, stream);
+}
+
+int gemv_ar_q8_round(gemv_ar_q8_t h, const void* x, int64_t ldx, int64_t rows, int8_t* xq, float* xs, hipStream_t stream) {
+  if (int rc = check_plan(h)) return rc;
+  if (rows < 0 || rows > INT_MAX) return fail(EBAG_EINVAL, "rows=%lld outside [0, 2^31)", (long long)rows);
+  if (!rows) return EBAG_OK;
+  if (!x) return fail(EBAG_EINVAL, "null x");
+  if (int rc = check_x(h, x, ldx, xq, xs)) return rc;
+  return launch_round(h, x, ldx, rows, xq, xs, stream);
+}
+
+int gemv_ar_q8_forward(gemv_ar_q8_t h, const int8_t* codes, const float* scales, const void* x, int64_t ldx, int64_t rows,
+                       int8_t* xq, float* xs, void* y, int64_t ldy, int32_t y_dtype, hipStream_t stream) {
+  if (int rc = check_plan(h)) return rc;
+  if (rows < 0 || rows > INT_MAX) return fail(EBAG_EINVAL, "rows=%lld outside [0, 2^31)", (long long)rows);
+  if (!rows) return EBAG_OK;
+  Q8Args a;
+  if (int rc = fill_args(h, codes, scales, x, ldx, rows, xq, xs, rows, y, ldy, y_dtype, &a)) return rc;
+  if (x)
+    if (int rc = launch_round(h, x, ldx, rows, xq, xs, stream)) return rc;
+  return launch(a, stream);
+}
+
+int gemv_ar_q8_experts(gemv_ar_q8_t h, const int8_t* codes, const float* scales, const void* x, int64_t ldx, int64_t x_rows,
+                       int8_t* xq, float* xs, const int32_t* offsets, const int32_t* src, int32_t choices, int64_t rows,
+                       void* y, int64_t ldy, int32_t y_dtype, hipStream_t stream) {
+  if (int rc = check_plan(h)) return rc;
+  if (rows < 0 || rows > INT_MAX) return fail(EBAG_EINVAL, "rows=%lld outside [0, 2^31)", (long long)rows);
+  if (!rows) return EBAG_OK;
+  if (!offsets) return fail(EBAG_EINVAL, "null offsets");
+  if (src && choices < 1) return fail(EBAG_EINVAL, "choices=%d must be positive", choices);
+  if (x_rows < 1 || x_rows > INT_MAX || (!src && x_rows != rows))
+    return fail(EBAG_EINVAL, "x_rows=%lld: without src x has as many rows as y", (long long)x_rows);
+  Q8Args a;
+  if (int rc = fill_args(h, codes, scales, x, ldx, x_rows, xq, xs, rows, y, ldy, y_dtype, &a)) return rc;
+  a.offsets = offsets;
+  a.src = src;
+  a.by_choices = make_divisor(src ? choices : 1);
+  if (x)
+    if (int rc = launch_round(h, x, ldx, x_rows, xq, xs, stream)) return rc;
+  return launch(a, stream);
+}
+
+void gemv_ar_q8_destroy(gemv_ar_q8_t h) { delete h; }
+
+}  // extern "C"
