@@ -60,9 +60,12 @@ __device__ __forceinline__ void q8_store(const Q8Args& a, uint32_t n, int64_t m,
     reinterpret_cast<__bf16*>(p)[m] = Type<2>::narrow(v);
 }
 
-constexpr int kQ8TileRows = 256;  // rows of weights of a workgroup of the matrix-product kernel
+// Rows of weights and rows of x of a workgroup of the matrix-product kernel.
+enum Q8Tile { Q8_256x64, Q8_512x128, Q8_256x256 };
+constexpr int q8_tile_w(Q8Tile t) { return t == Q8_512x128 ? 512 : 256; }
+constexpr int q8_tile_x(Q8Tile t) { return t == Q8_256x64 ? 64 : t == Q8_512x128 ? 128 : 256; }
 
 void launch_q8_few(const Q8Args& a, int tiles, int x_tiles, unsigned grid, int threads, hipStream_t stream);
-void launch_q8_tile(const Q8Args& a, int x_rows, unsigned grid, hipStream_t stream);
+void launch_q8_tile(const Q8Args& a, Q8Tile kind, unsigned grid, hipStream_t stream);
 
 }  // namespace ebag

@@ -240,14 +240,15 @@ int launch_few(Q8Args a, int x_tiles, hipStream_t stream) {
   return e == hipSuccess ? EBAG_OK : hipf(e, "launch the product in 8 bits");
 }
 
-int launch_tile(Q8Args a, int x_rows, hipStream_t stream) {
-  const int64_t per_wg = kQ8TileRows / (a.glu ? 2 : 1), tiles = (a.out_rows + per_wg - 1) / per_wg;
+int launch_tile(Q8Args a, Q8Tile kind, hipStream_t stream) {
+  const int x_rows = q8_tile_x(kind);
+  const int64_t per_wg = q8_tile_w(kind) / (a.glu ? 2 : 1), tiles = (a.out_rows + per_wg - 1) / per_wg;
   const int64_t slots = a.offsets ? most_tiles(a.rows, a.experts, x_rows) : (a.rows + x_rows - 1) / x_rows;
   const int64_t grid = (slots + 3) / 4 * 4 * tiles;
   if (grid > INT_MAX) return fail(EBAG_EUNSUPPORTED, "too many tiles for one launch");
   a.by_tiles = make_divisor(tiles);
   a.whole = (uint32_t)(grid / 256 * 256);
-  launch_q8_tile(a, x_rows, (unsigned)grid, stream);
+  launch_q8_tile(a, kind, (unsigned)grid, stream);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? EBAG_OK : hipf(e, "launch the product in 8 bits");
 }
@@ -257,7 +258,7 @@ int launch(const Q8Args& a, hipStream_t stream) {
   if (each <= 16) return launch_few(a, 1, stream);
   if (each <= 32) return launch_few(a, 2, stream);
   if (each <= 64) return launch_few(a, 4, stream);
-  return launch_tile(a, each <= 128 ? 64 : each <= 1024 ? 128 : 256, stream);
+  return launch_tile(a, each <= 128 ? Q8_256x64 : each <= 1024 ? Q8_512x128 : Q8_256x256, stream);
 }
 
 }  // namespace
