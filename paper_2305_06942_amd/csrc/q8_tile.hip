@@ -11,18 +11,32 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kStep = kQ8Line;  // columns of a step
-constexpr int kSlices = kStep / 32;
 
-// WW x WX waves, four in all, have 32 TW rows of weights and 32 TX rows of x each.  Both go
+// Sums stay where they are.  With the compiler's builtin, whose sums may move, it moves them: 264 moves a step (8192 x
+// 8192 x 8192: 778 us, like this 412).  What the compiler then does not see are the wait states between a matrix
+// instruction and others on its sums: settle() keeps them, behind the first values and ahead of the results' use.
+__device__ __forceinline__ void add_product(i32x4& sum, const i32x4& w, const i32x4& x) {
+  asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, %0" : "+a"(sum) : "v"(w), "v"(x));
+}
+template <int N>
+__device__ __forceinline__ void settle(i32x4 (&sum)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+a"(sum[i]));
+  asm volatile("s_nop 15\n\ts_nop 15");
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+a"(sum[i]));
+}
+
+// WW x WX waves, four in all, have 16 TW rows of weights and 16 TX rows of x each.  Both go
 // through LDS, two steps of 128 columns in turn, 16-byte pieces of a row exchanged by
 // its number so that the lanes of an operand find theirs on different banks.
-template <int WW, int WX, int TW, int TX, bool GLU, int ELT>
+template <int WW, int WX, int TW, int TX, bool GLU, int DT>
 __global__ __launch_bounds__(kThreads, 1) void q8_tile_kernel(const Q8Args a) {
-  constexpr int BW = 32 * TW * WW, BX = 32 * TX * WX, ROWS = BW + BX;
+  constexpr int BW = 16 * TW * WW, BX = 16 * TX * WX, ROWS = BW + BX;
   constexpr int W_STAGED = BW / 32, STAGED = ROWS / 32;  // pieces of a thread, 32 rows apart
   constexpr int BUFFER = ROWS * kStep;
   extern __shared__ __attribute__((aligned(16))) char lds[];
-  const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, r32 = lane & 31;
+  const int tid = threadIdx.x, lane = tid & 63, quarter = lane >> 4, r16 = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wave_w = wave % WW, wave_x = wave / WW;
   // 32 neighbouring tiles to each XCD, whose L2 then has what they share.
   uint32_t block = blockIdx.x;
@@ -65,78 +79,72 @@ __global__ __launch_bounds__(kThreads, 1) void q8_tile_kernel(const Q8Args a) {
     x_from[i] = a.xq + q8_x_row(a, n) * a.pitch + chunk * 16;
   }
   char* to = lds + row0 * kStep + (chunk ^ (row0 >> 1 & 7)) * 16;  // rows 32 apart have the same exchange
-  const char* w_lds = lds + (wave_w * (32 * TW) + r32) * kStep;
-  const char* x_lds = lds + (BW + wave_x * (32 * TX) + r32) * kStep;
-  const int turn = r32 >> 1 & 7;
+  const char* w_lds = lds + (wave_w * (16 * TW) + r16) * kStep;
+  const char* x_lds = lds + (BW + wave_x * (16 * TX) + r16) * kStep;
+  const int turn = r16 >> 1 & 7;
 
-  i32x16 sum[TW][TX];
+  i32x4 sum[TW][TX];
 #pragma unroll
   for (int b = 0; b < TW; ++b)
 #pragma unroll
-    for (int t = 0; t < TX; ++t)
+    for (int t = 0; t < TX; ++t) sum[b][t] = i32x4{0, 0, 0, 0};
 #pragma unroll
-      for (int i = 0; i < 16; ++i) sum[b][t][i] = 0;
+  for (int b = 0; b < TW; ++b) settle(sum[b]);
 
   vec16 staged[STAGED];
-  struct Operands {
-    i32x4 w[TW], x[TX];
-  };
-  Operands even, odd;
+  i32x4 w_now[TW], x_now[2][2];  // a slice's weights; two tiles of x, and the next two
   auto load = [&](int i, int step) {
     const int64_t at = (int64_t)step * kStep;
     staged[i] = load16(i < W_STAGED ? reinterpret_cast<const char*>(w_from + (i & 1 ? up : 0) + at) + w_at[i < W_STAGED ? i : 0]
                                     : reinterpret_cast<const char*>(x_from[i < W_STAGED ? 0 : i - W_STAGED] + at));
   };
   auto store = [&](int i, int buffer) { *reinterpret_cast<vec16*>(to + buffer * BUFFER + i * 32 * kStep) = staged[i]; };
-  // Operand number i, in the order in which the products need them.
-  auto fetch = [&](Operands& o, int buffer, int slice, int i) {
-    const int piece = ((slice * 2 + half) ^ turn) * 16 + buffer * BUFFER;
-    if (i > 0 && i <= TW)
-      o.w[i > 0 && i <= TW ? i - 1 : 0] = *reinterpret_cast<const i32x4*>(w_lds + 32 * (i - 1) * kStep + piece);
-    else
-      o.x[i ? i - TW : 0] = *reinterpret_cast<const i32x4*>(x_lds + 32 * (i ? i - TW : 0) * kStep + piece);
+  auto piece_of = [&](int buffer, int slice) { return ((slice * 4 + quarter) ^ turn) * 16 + buffer * BUFFER; };
+  auto fetch_w = [&](int b, int piece) { w_now[b] = *reinterpret_cast<const i32x4*>(w_lds + 16 * b * kStep + piece); };
+  auto fetch_x = [&](int t, int piece) {
+    x_now[t / 2 & 1][t & 1] = *reinterpret_cast<const i32x4*>(x_lds + 16 * t * kStep + piece);
   };
-  // A slice's products, with other work between them: kept where it stands, so that a wave alone on its SIMD always
-  // has products under way while it waits for memory.
-  constexpr int GROUPS = TW + TX, EACH = TW * TX / GROUPS;
-  static_assert(EACH * GROUPS == TW * TX, "");
-  auto multiply = [&](const Operands& o, auto other) __attribute__((always_inline)) {
+  // A slice's products, two tiles of x at a time with each of weights in turn, and behind every two products what is to
+  // be done besides: kept where it stands, so that a wave alone on its SIMD always has products under way while it
+  // waits for memory.  The next two tiles of x are fetched meanwhile, and with the last two the next slice's weights,
+  // into the registers of those that have no more products: both 2 TW products ahead of their use.
+  constexpr int GROUPS = TX / 2 * TW;
+  static_assert(TX % 4 == 0, "a slice's first tiles of x are in the first registers");
+  auto multiply = [&](auto fetches, int piece, int next, auto other) __attribute__((always_inline)) {
 #pragma unroll
     for (int g = 0; g < GROUPS; ++g) {
-#pragma unroll
-      for (int i = g * EACH; i < (g + 1) * EACH; ++i)
-        sum[i % TW][i / TW] = __builtin_amdgcn_mfma_i32_32x32x32_i8(o.w[i % TW], o.x[i / TW], sum[i % TW][i / TW], 0, 0, 0);
+      const int t = g / TW * 2, b = g % TW;
       other(g);
+      add_product(sum[b][t], w_now[b], x_now[t / 2 & 1][0]);
+      add_product(sum[b][t + 1], w_now[b], x_now[t / 2 & 1][1]);
+      const bool last = t == TX - 2;
+      if (!last && b < 2) fetch_x(t + 2 + b, piece);
+      if (last && decltype(fetches)::value) {
+        fetch_w(b, next);
+        if (b < 2) fetch_x(b, next);
+      }
       __builtin_amdgcn_sched_barrier(0);
     }
   };
   // One step's products.  Its first operands are in registers; the next step's rows, loaded a step ago, go to the
-  // other buffer, which nobody reads any more, while the second and third slices are multiplied, and the loads of the
-  // step after that take their registers.  After the third slice every wave has read what it needs of this buffer and
-  // stored its part of the other: one barrier a step, with a slice's products to follow at once.
+  // other buffer, which nobody reads any more, and the loads of the step after that take their registers.  When the
+  // last two tiles of x have their turn, every wave has what it needs of this buffer and has stored its part of the
+  // other: one barrier a step, with products to follow at once.
   auto work = [&](int buffer, int step, auto stores, auto loads) __attribute__((always_inline)) {
     constexpr bool STORES = decltype(stores)::value, LOADS = decltype(loads)::value;
-    auto move = [&](int part, int g) __attribute__((always_inline)) {  // the pieces between whose products this group is
-      constexpr int MOVES = 2 * GROUPS;
-      const int from = (part * GROUPS + g) * STAGED / MOVES, to = (part * GROUPS + g + 1) * STAGED / MOVES;
+    constexpr int MOVES = 2 * GROUPS - TW;  // groups with room for moves
+    auto move = [&](int g) __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = from; i < to; ++i) {
+      for (int i = g * STAGED / MOVES; i < (g + 1) * STAGED / MOVES; ++i) {
         if (STORES) store(i, buffer ^ 1);
         if (LOADS) load(i, step + 2);
       }
     };
-    multiply(even, [&](int g) __attribute__((always_inline)) { fetch(odd, buffer, 1, g); });
-    multiply(odd, [&](int g) __attribute__((always_inline)) {
-      fetch(even, buffer, 2, g);
-      move(0, g);
-    });
-    multiply(even, [&](int g) __attribute__((always_inline)) {
-      fetch(odd, buffer, 3, g);
-      move(1, g);
-    });
-    __syncthreads();
-    multiply(odd, [&](int g) __attribute__((always_inline)) {
-      if (STORES) fetch(even, buffer ^ 1, 0, g);
+    const int second = piece_of(buffer, 1), next = piece_of(buffer ^ 1, 0);
+    multiply(std::true_type(), piece_of(buffer, 0), second, move);
+    multiply(stores, second, next, [&](int g) __attribute__((always_inline)) {
+      if (g < GROUPS - TW) move(GROUPS + g);
+      if (STORES && g == GROUPS - TW) __syncthreads();
     });
   };
   const int steps = (int)(a.pitch / kStep);
@@ -153,88 +161,92 @@ __global__ __launch_bounds__(kThreads, 1) void q8_tile_kernel(const Q8Args a) {
   }
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < GROUPS; ++i) fetch(even, 0, 0, i);
+  for (int b = 0; b < TW; ++b) fetch_w(b, piece_of(0, 0));
+#pragma unroll
+  for (int t = 0; t < 2; ++t) fetch_x(t, piece_of(0, 0));
   int step = 0;
   for (; step + 2 < steps; ++step) work(step & 1, step, std::true_type(), std::true_type());
   if (step + 1 < steps) {
     work(step & 1, step, std::true_type(), std::false_type());
     ++step;
   }
-  work(step & 1, step, std::false_type(), std::false_type());
-
-  // A lane has row r32 of x and, in element i, weight row 8 (i / 4) + 4 half + i % 4: four neighbours, which go to LDS
-  // as one piece, 32 rows of x at a time, and from there to y in whole rows.
-  constexpr int COLS = 32 * TW / pair, PITCH = COLS * ELT + 16;  // columns of y that the wave has; bytes of a row in LDS
+  // A lane has row r16 of x and weight rows 4 quarter ...: four neighbours, which go to LDS as one piece, 32 rows of x at
+  // a time, and from there to y in whole rows.  With glu tiles 0 and 1 of every four are of gate rows, 2 and 3 of up rows.
+  // The scales are loaded ahead of the last step's products.
+  constexpr int ELT = DT == 0 ? 4 : 2;
+  constexpr int COLS = 16 * TW / pair, PITCH = COLS * ELT + 16;  // columns of y that the wave has; bytes of a row in LDS
   constexpr int VEC = 16 / ELT, PER_ROW = COLS / VEC;            // elements of a vector, vectors of a row
   const int64_t m0 = wg_m0 + wave_w * COLS;
   const int64_t left = a.out_rows - m0;                          // columns of y from the wave's first on
   const float* scales = a.scales + (int64_t)expert * a.M;
-  float ws[TW][16], xs[TX];
+  auto col_of = [&](int b) { return (GLU ? b / 4 * 2 + b % 2 : b) * 16 + 4 * quarter; };
+  float ws[TW][4], xs[TX];
 #pragma unroll
-  for (int b = 0; b < TW; ++b)
+  for (int b = 0; b < TW; ++b) {
+    const int col = col_of(b);
+    const float* from = scales + (GLU && b % 4 >= 2 ? a.out_rows : 0);
+    if (col + 4 <= left) {
+      Type<0>::widen(load16(reinterpret_cast<const char*>(from + m0 + col)), ws[b]);
+    } else {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int col = (GLU ? b / 2 : b) * 32 + 8 * q + 4 * half;
-      const float* from = scales + (GLU && b % 2 ? a.out_rows : 0);
-      if (col + 4 <= left) {
-        Type<0>::widen(load16(reinterpret_cast<const char*>(from + m0 + col)), &ws[b][4 * q]);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) ws[b][4 * q + i] = from[col + i < left ? m0 + col + i : a.out_rows - 1];
-      }
+      for (int i = 0; i < 4; ++i) ws[b][i] = from[col + i < left ? m0 + col + i : a.out_rows - 1];
     }
+  }
 #pragma unroll
   for (int t = 0; t < TX; ++t) {
-    const uint32_t n = first + wave_x * (32 * TX) + 32 * t + r32;
+    const uint32_t n = first + wave_x * (16 * TX) + 16 * t + r16;
     xs[t] = a.xs[q8_x_row(a, n < end ? n : end - 1)];
   }
+  work(step & 1, step, std::false_type(), std::false_type());
+#pragma unroll
+  for (int b = 0; b < TW; ++b) settle(sum[b]);
+
   __syncthreads();
   char* mine = lds + wave * (32 * PITCH);
 #pragma unroll
-  for (int t = 0; t < TX; ++t) {
-    const uint32_t n0 = first + wave_x * (32 * TX) + 32 * t;
+  for (int t0 = 0; t0 < TX; t0 += 2) {
+    const uint32_t n0 = first + wave_x * (16 * TX) + 16 * t0;
     if (n0 >= end) break;
 #pragma unroll
-    for (int b = 0; b < TW; b += pair)
+    for (int t = t0; t < t0 + 2; ++t)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
+      for (int b = 0; b < TW; ++b) {
+        if (GLU && b % 4 >= 2) continue;
         float v[8] = {};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int at = 4 * q + i;
-          v[i] = (float)sum[b][t][at] * (xs[t] * ws[b][at]);
-          if (GLU) v[i] = silu<ELT == 4>(v[i]) * ((float)sum[b + pair - 1][t][at] * (xs[t] * ws[b + pair - 1][at]));
+          v[i] = (float)sum[b][t][i] * (xs[t] * ws[b][i]);
+          if (GLU) v[i] = silu<DT == 0>(v[i]) * ((float)sum[GLU ? b + 2 : b][t][i] * (xs[t] * ws[GLU ? b + 2 : b][i]));
         }
-        char* to = mine + r32 * PITCH + (b / pair * 32 + 8 * q + 4 * half) * ELT;
-        if constexpr (ELT == 4) {
-          *reinterpret_cast<vec16*>(to) = Type<0>::narrow(v);
-        } else {
-          const vec16 p = a.y_type == EBAG_F16 ? Type<1>::narrow(v) : Type<2>::narrow(v);
+        char* to = mine + ((t - t0) * 16 + r16) * PITCH + col_of(b) * ELT;
+        const vec16 p = Type<DT>::narrow(v);
+        if constexpr (DT == 0)
+          *reinterpret_cast<vec16*>(to) = p;
+        else
           *reinterpret_cast<uint2*>(to) = uint2{p[0], p[1]};
-        }
       }
     __builtin_amdgcn_wave_barrier();
     constexpr int LANES = PER_ROW < 64 ? PER_ROW : 64;  // of a row
     const int r0 = lane / LANES, c = lane % LANES * VEC;
     char* out = a.y + (int64_t)(n0 + r0) * a.ldy + (m0 + c) * ELT;
     const char* at = mine + r0 * PITCH + c * ELT;
-    if (c < left) {
+    constexpr int ROUND = 64 / LANES;  // rows at a time
+    if (n0 + 32 <= end && COLS <= left) {
 #pragma unroll
-      for (int i = 0; i < LANES / 2; ++i) {
-        if (n0 + r0 + i * (64 / LANES) >= end) break;
-        char* row = out + (int64_t)i * (64 / LANES) * a.ldy;
-        const vec16 v = *reinterpret_cast<const vec16*>(at + i * (64 / LANES) * PITCH);
-        if (c + VEC <= left) {
-          store16(row, v);
+      for (int i = 0; i < 32 / ROUND; ++i)
+        store16(out + (int64_t)(i * ROUND) * a.ldy, *reinterpret_cast<const vec16*>(at + i * ROUND * PITCH));
+    } else {
+      const int64_t fit = left - c;
+#pragma unroll 1
+      for (int i = 0; i < 32 && n0 + r0 + i < end && fit > 0; i += ROUND) {
+        char* row = out + i * a.ldy;
+        const char* from = at + i * PITCH;
+        if (fit >= VEC) {
+          store16(row, *reinterpret_cast<const vec16*>(from));
         } else {
-#pragma unroll
-          for (int e = 0; e < VEC; ++e)
-            if (c + e < left) {
-              if constexpr (ELT == 4)
-                reinterpret_cast<uint32_t*>(row)[e] = v[e];
-              else
-                reinterpret_cast<uint16_t*>(row)[e] = (uint16_t)(e & 1 ? v[e / 2] >> 16 : v[e / 2] & 0xffffu);
-            }
+#pragma unroll 1
+          for (int e = 0; e < fit; ++e)
+            reinterpret_cast<typename Type<DT>::elt*>(row)[e] = reinterpret_cast<const typename Type<DT>::elt*>(from)[e];
         }
       }
     }
@@ -244,21 +256,21 @@ __global__ __launch_bounds__(kThreads, 1) void q8_tile_kernel(const Q8Args a) {
 
 template <int WW, int WX, int TW, int TX>
 void launch(const Q8Args& a, unsigned grid, hipStream_t stream) {
-  constexpr size_t stages = 2 * (size_t)(32 * TW * WW + 32 * TX * WX) * kStep, out = 4 * 32 * (32 * TW * 4 + 16);
-  const bool f32 = a.y_type == EBAG_F32;
-  hipLaunchKernelGGL((a.glu ? f32 ? q8_tile_kernel<WW, WX, TW, TX, true, 4> : q8_tile_kernel<WW, WX, TW, TX, true, 2>
-                      : f32 ? q8_tile_kernel<WW, WX, TW, TX, false, 4>
-                            : q8_tile_kernel<WW, WX, TW, TX, false, 2>),
-                     dim3(grid), dim3(kThreads), stages > out ? stages : out, stream, a);
+  constexpr size_t stages = 2 * (size_t)(16 * TW * WW + 16 * TX * WX) * kStep, out = 4 * 32 * (16 * TW * 4 + 16);
+  void (*fn)(const Q8Args) = a.y_type == EBAG_F32   ? a.glu ? q8_tile_kernel<WW, WX, TW, TX, true, 0> : q8_tile_kernel<WW, WX, TW, TX, false, 0>
+                             : a.y_type == EBAG_F16 ? a.glu ? q8_tile_kernel<WW, WX, TW, TX, true, 1> : q8_tile_kernel<WW, WX, TW, TX, false, 1>
+                             : a.glu                ? q8_tile_kernel<WW, WX, TW, TX, true, 2>
+                                                    : q8_tile_kernel<WW, WX, TW, TX, false, 2>;
+  hipLaunchKernelGGL(fn, dim3(grid), dim3(kThreads), stages > out ? stages : out, stream, a);
 }
 
 }  // namespace
 
 void launch_q8_tile(const Q8Args& a, Q8Tile kind, unsigned grid, hipStream_t stream) {
   switch (kind) {
-    case Q8_256x256: return launch<2, 2, 4, 4>(a, grid, stream);
-    case Q8_512x128: return launch<4, 1, 4, 4>(a, grid, stream);
-    default: return launch<4, 1, 2, 2>(a, grid, stream);
+    case Q8_256x256: return launch<2, 2, 8, 8>(a, grid, stream);
+    case Q8_512x128: return launch<4, 1, 8, 8>(a, grid, stream);
+    default: return launch<4, 1, 4, 4>(a, grid, stream);
   }
 }
 
