@@ -38,8 +38,6 @@ struct Q8Args {
   int32_t y_type;
   Divisor by_choices;
   Divisor by_tiles;         // workgroups that share the rows of x, each with its rows of weights
-  // The kernel for few rows.
-  int32_t split;            // waves that share a tile
   // The matrix-product kernel.
   uint32_t whole;           // workgroups in whole rounds of all XCDs
 };
@@ -65,7 +63,8 @@ enum Q8Tile { Q8_256x64, Q8_512x128, Q8_256x256 };
 constexpr int q8_tile_w(Q8Tile t) { return t == Q8_512x128 ? 512 : 256; }
 constexpr int q8_tile_x(Q8Tile t) { return t == Q8_256x64 ? 64 : t == Q8_512x128 ? 128 : 256; }
 
-void launch_q8_few(const Q8Args& a, int tiles, int x_tiles, unsigned grid, int threads, hipStream_t stream);
+// tiles: of 16 rows of weights of a wave; x_tiles: of 16 rows of x; waves: of four, that have different rows of weights.
+void launch_q8_few(const Q8Args& a, int tiles, int x_tiles, int waves, unsigned grid, hipStream_t stream);
 void launch_q8_tile(const Q8Args& a, Q8Tile kind, unsigned grid, hipStream_t stream);
 
 }  // namespace ebag

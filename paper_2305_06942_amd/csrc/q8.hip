@@ -7,6 +7,7 @@
 
 #include "ebag_a2a.h"
 #include "gemv_ar.h"
+#include "lanes.h"
 #include "q8.h"
 
 using namespace ebag;
@@ -31,13 +32,20 @@ struct RoundArgs {
 
 // The largest over the 64 lanes, in each of them; of numbers without a sign, as whole numbers keep the order of
 // floats and put NaN above infinity.
+__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return a > b ? a : b; }
+template <int CTRL>
+__device__ __forceinline__ uint32_t larger_dpp(uint32_t v) {
+  return larger(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true));
+}
 __device__ __forceinline__ uint32_t largest(uint32_t v) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const uint32_t o = __shfl_xor(v, d);
-    v = v > o ? v : o;
-  }
-  return v;
+  v = larger_dpp<0xB1>(v);
+  v = larger_dpp<0x4E>(v);
+  v = larger_dpp<0x141>(v);
+  v = larger_dpp<0x140>(v);
+  const u32x2 s = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = larger(s[0], s[1]);
+  const u32x2 t = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return larger(t[0], t[1]);
 }
 
 // Eight neighbouring elements in fp32, zeros behind the row's end.
@@ -179,7 +187,7 @@ int launch_round(const gemv_ar_q8_plan* h, const void* x, int64_t ldx, int64_t r
   a.rows = rows;
   a.K = (int32_t)h->K;
   a.units = (int32_t)(h->pitch / 8);
-  const bool wave = h->K <= 64 * 8 * kHeld;
+  const bool wave = h->K <= 64 * 8 * kHeld && (rows >= 2048 || h->K <= 256);
   const int64_t per_wg = wave ? kRoundThreads / 64 : 1, wgs = (rows + per_wg - 1) / per_wg;
   if (wgs > INT_MAX) return fail(EBAG_EUNSUPPORTED, "too many rows for one launch");
   void (*fn)(const RoundArgs) = h->dtype == EBAG_F32   ? wave ? q8_round_kernel<0, true> : q8_round_kernel<0, false>
@@ -222,20 +230,22 @@ int fill_args(const gemv_ar_q8_plan* h, const int8_t* codes, const float* scales
   return EBAG_OK;
 }
 
+// Waves with different rows of weights: as many as leave every CU a workgroup, since they share x; the others share the
+// columns (bf16, in us by 1, 2, 4 and 8 of them: 16 rows x 4096 x 4096 6.7, 7.7; x 14336 x 4096 16.8, 13.1; x 65536 x 8192
+// 103, 92; 32 rows 8.0, 10.0, 12.7; 20.6, 15.2, 14.7; 135, 104, 95; 64 rows 11.3, 12.7, 17.5, 20.3; 40, 20.3, 19.4, 22.2;
+// 238, 136, 109, 97).  One tile of weights to a wave; two, for glu, take 1 to 30 % longer.  Where few workgroups have
+// much of K each, eight waves share it.
 int launch_few(Q8Args a, int x_tiles, hipStream_t stream) {
   const int cols = 16 * x_tiles;
   const int64_t slots = a.offsets ? most_tiles(a.rows, a.experts, cols) : (a.rows + cols - 1) / cols;
-  const int64_t singles = (a.out_rows + 15) / 16 * slots;  // tiles of 16 columns of y
-  const int tiles = a.glu || singles >= 4096 ? 2 : 1;
-  const int64_t wave_cols = a.glu ? 16 : 16 * tiles;
-  const int64_t all_tiles = (a.out_rows + wave_cols - 1) / wave_cols * slots, lines = a.pitch / kQ8Line;
-  a.split = 1;
-  while (a.split < 8 && all_tiles * a.split < 4096 && lines >= 4 * a.split) a.split *= 2;
-  const int waves = a.split > 4 ? 8 : 4;
-  const int64_t wg_cols = wave_cols * (waves / a.split), grid_tiles = (a.out_rows + wg_cols - 1) / wg_cols;
+  const int64_t wave_tiles = (a.out_rows + 15) / 16, used = a.offsets ? (a.rows + cols - 1) / cols : slots;
+  const int most = x_tiles == 1 ? 2 : x_tiles == 2 ? 4 : 8;
+  int waves = 1;
+  while (waves < most && wave_tiles * used >= 200 * 2 * waves) waves *= 2;
+  const int64_t grid_tiles = (wave_tiles + waves - 1) / waves;
   if (grid_tiles * slots > INT_MAX) return fail(EBAG_EUNSUPPORTED, "too many tiles for one launch");
   a.by_tiles = make_divisor(grid_tiles);
-  launch_q8_few(a, tiles, x_tiles, (unsigned)(grid_tiles * slots), 64 * waves, stream);
+  launch_q8_few(a, a.glu ? 2 : 1, x_tiles, waves, (unsigned)(grid_tiles * slots), stream);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? EBAG_OK : hipf(e, "launch the product in 8 bits");
 }

@@ -7,92 +7,141 @@
 namespace ebag {
 namespace {
 
-// A wave has RT tiles of 16 rows of weights (with glu a tile of gate rows and the up rows
-// that go with them) and NT tiles of 16 rows of x, and of their columns the part that is
-// its of `split` waves.  Weights and x come straight from memory into the operands'
-// registers, two lines of each row at a time and the next two on their way; sums are
-// whole numbers, so the order in which the waves' parts are joined does not matter.
-template <int RT, int NT>
-__global__ __launch_bounds__(512) void q8_few_kernel(const Q8Args a) {
+constexpr int kCuLds = 160 * 1024;
+
+// 16 bytes of each lane from memory into LDS, `to` and behind, without a register between: the wave may have as many
+// under way as there is LDS for them.  The compiler's own builtin would have every later load from LDS wait for all of
+// them; here the kernel waits itself (arrived()), by their number, as they arrive in order.
+__device__ __forceinline__ void copy_to_lds(uint32_t to, const int8_t* from) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory");
+}
+// Waits until at most N copies of this wave are under way, and for the other waves to have come as far.
+template <int N>
+__device__ __forceinline__ void arrived() {
+  static_assert(N <= 63, "");
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+// Of a workgroup's WAVES waves WW have different rows of weights, RT tiles of 16 each (with glu tiles of gate rows
+// and the up rows that go with them), and WK = WAVES / WW share the columns, each a part of whole lines of 128.  All of
+// them have the same NT tiles of 16 rows of x.  A line of each row goes through LDS, in a ring of STAGES of them.
+// Sums are whole numbers, so the order in which the parts of the columns are joined does not matter.
+template <int RT, int NT, int WW, int WAVES>
+struct Few {
+  static constexpr int WK = WAVES / WW;
+  static constexpr int W_ROWS = 16 * RT * WW, X_ROWS = 16 * NT, ROWS = W_ROWS + X_ROWS;  // of a part of the columns
+  static constexpr int STAGE = WK * ROWS * (int)kQ8Line;
+  static constexpr int X_COPIES = X_ROWS / 8 / WW, COPIES = 2 * RT + X_COPIES;           // of a wave, eight rows each
+  static_assert(X_COPIES * 8 * WW == X_ROWS, "");
+  // Three workgroups on a CU, or two, or one.
+  static constexpr int RING = kCuLds / (STAGE * 9 <= kCuLds ? 3 : STAGE * 6 <= kCuLds ? 2 : 1);
+  static constexpr int FIT = RING / STAGE, MOST = 62 / COPIES + 2;
+  static constexpr int STAGES = FIT < MOST ? FIT : MOST;
+  static_assert(STAGES >= 3, "");
+  static constexpr int JOIN = WAVES * RT * NT * 64 * 16;
+  static constexpr int LDS = STAGES * STAGE > JOIN ? STAGES * STAGE : JOIN;
+};
+
+template <int RT, int NT, int WW, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void q8_few_kernel(const Q8Args a) {
+  typedef Few<RT, NT, WW, WAVES> F;
   extern __shared__ __attribute__((aligned(16))) char lds[];
-  constexpr int P = 2;  // lines at a time
   const int lane = threadIdx.x & 63, r16 = lane & 15, quarter = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int waves = blockDim.x >> 6, split = a.split, part = wave & (split - 1), own = wave / split;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave_w = wave % WW, part = wave / WW;
   const uint32_t slot = divide_by(a.by_tiles, blockIdx.x), tile = blockIdx.x - slot * a.by_tiles.d;
   int expert;
   uint32_t first, end;
   if (!find_tile(a, slot, 16 * NT, &expert, &first, &end)) return;
-  const int pair = a.glu ? 2 : 1;
-  const int64_t wg_cols = 16 * RT / pair * (waves / split);
-  const int64_t m0 = tile * wg_cols + own * (16 * RT / pair);
+  const int pair = RT > 1 && a.glu ? 2 : 1;
+  const int wave_cols = 16 * RT / pair;  // of y
+  const int64_t wg_m0 = (int64_t)tile * (wave_cols * WW), m0 = wg_m0 + wave_w * wave_cols;
   if (expert == a.experts) {
-    for (uint32_t i = threadIdx.x; i < 16u * NT * (uint32_t)wg_cols; i += blockDim.x) {
-      const uint32_t n = first + i / (uint32_t)wg_cols;
-      const int64_t m = tile * wg_cols + i % (uint32_t)wg_cols;
+    const uint32_t cols = wave_cols * WW;
+    for (uint32_t i = threadIdx.x; i < F::X_ROWS * cols; i += 64 * WAVES) {
+      const uint32_t n = first + i / cols;
+      const int64_t m = wg_m0 + i % cols;
       if (n < end && m < a.out_rows) q8_store(a, n, m, 0.f);
     }
     return;
   }
-  const int8_t* w[RT];
-  const int8_t* x[NT];
+  // Copies: eight rows at a time, eight lanes to a row.  A lane's 16 bytes go to its place in the row, so they come from
+  // where that place's are: pieces are exchanged by half the row's number, for the operands' loads to find them on
+  // different banks.
+  const int row8 = lane >> 3;
+  const int8_t* from[F::COPIES];
+  uint32_t to[F::COPIES];
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds + part * (F::ROWS * (int)kQ8Line);
 #pragma unroll
-  for (int b = 0; b < RT; ++b) {
-    int64_t m = m0 + (pair == 2 ? 0 : 16 * b) + r16;
-    m = m < a.out_rows ? m : a.out_rows - 1;
-    w[b] = a.codes + ((int64_t)expert * a.M + (pair == 2 && b ? a.out_rows : 0) + m) * a.pitch + quarter * 16;
-  }
-#pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    uint32_t n = first + 16 * t + r16;
-    n = n < end ? n : end - 1;
-    x[t] = a.xq + q8_x_row(a, n) * a.pitch + quarter * 16;
-  }
-  const int lines = (int)(a.pitch / kQ8Line);
-  const int from = lines * part / split, to = lines * (part + 1) / split;
-  struct Lines {
-    i32x4 w[RT][2 * P], x[NT][2 * P];
-  };
-  auto load = [&](Lines& l, int line) {
-#pragma unroll
-    for (int p = 0; p < P; ++p) {
-      const int64_t at = (int64_t)(line + p < to ? line + p : to - 1) * kQ8Line;  // a line again where there is none
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-#pragma unroll
-        for (int b = 0; b < RT; ++b) l.w[b][2 * p + h] = __builtin_bit_cast(i32x4, load16(reinterpret_cast<const char*>(w[b] + at + 64 * h)));
-#pragma unroll
-        for (int t = 0; t < NT; ++t) l.x[t][2 * p + h] = __builtin_bit_cast(i32x4, load16(reinterpret_cast<const char*>(x[t] + at + 64 * h)));
-      }
+  for (int i = 0; i < F::COPIES; ++i) {
+    int row;  // of the part's rows in LDS
+    if (i < 2 * RT) {
+      const int r = i * 8 + row8;  // of the wave's weight rows
+      row = wave_w * (16 * RT) + r;
+      int64_t m = m0 + (pair == 2 ? r / 32 * 16 + r % 16 : r);
+      m = m < a.out_rows ? m : a.out_rows - 1;
+      if (pair == 2 && r % 32 >= 16) m += a.out_rows;
+      from[i] = a.codes + ((int64_t)expert * a.M + m) * a.pitch;
+    } else {
+      const int r = ((i - 2 * RT) * WW + wave_w) * 8 + row8;
+      row = F::W_ROWS + r;
+      uint32_t n = first + r;
+      n = n < end ? n : end - 1;
+      from[i] = a.xq + q8_x_row(a, n) * a.pitch;
     }
+    from[i] += ((lane & 7) ^ (row >> 1 & 7)) * 16;
+    to[i] = lds0 + __builtin_amdgcn_readfirstlane(row - row8) * (int)kQ8Line;
+  }
+  const int lines = (int)(a.pitch / kQ8Line), steps = (lines + F::WK - 1) / F::WK, line0 = part * steps;
+  // Not every workgroup begins with its first line: rows of a power of two bytes would have all of them ask the same
+  // memory channels at a time (16 rows x 65536 x 8192: 117 us, like this 92; each eight neighbours, on an XCD each, alike).
+  const int turn0 = (int)((blockIdx.x >> 3) % (uint32_t)steps);
+  auto line_of = [&](int step) { return line0 + (step + turn0 < steps ? step + turn0 : step + turn0 - steps); };
+  auto copy = [&](int step, int stage) __attribute__((always_inline)) {
+    const int at = line_of(step), line = at < lines ? at : lines - 1;  // one again where there is none
+#pragma unroll
+    for (int i = 0; i < F::COPIES; ++i) copy_to_lds(to[i] + stage * F::STAGE, from[i] + (int64_t)line * kQ8Line);
   };
+  const char* mine = lds + part * (F::ROWS * (int)kQ8Line) + r16 * (int)kQ8Line;
+  const int turn = r16 >> 1 & 7;
   i32x4 sum[RT][NT];
 #pragma unroll
   for (int b = 0; b < RT; ++b)
 #pragma unroll
     for (int t = 0; t < NT; ++t) sum[b][t] = i32x4{0, 0, 0, 0};
-  if (from < to) {
-    Lines now, next;
-    load(now, from);
-    for (int line = from; line < to; line += P) {
-      if (line + P < to) load(next, line + P);
+  auto multiply = [&](int stage) __attribute__((always_inline)) {
+    const char* rows = mine + stage * F::STAGE;
 #pragma unroll
-      for (int p = 0; p < P; ++p) {
-        if (line + p >= to) break;
+    for (int h = 0; h < 2; ++h) {
+      const int piece = ((h * 4 + quarter) ^ turn) * 16;
+      i32x4 w[RT], x[NT];
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+      for (int b = 0; b < RT; ++b) w[b] = *reinterpret_cast<const i32x4*>(rows + (wave_w * RT + b) * (16 * (int)kQ8Line) + piece);
 #pragma unroll
-          for (int b = 0; b < RT; ++b)
+      for (int t = 0; t < NT; ++t) x[t] = *reinterpret_cast<const i32x4*>(rows + (F::W_ROWS + 16 * t) * (int)kQ8Line + piece);
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
-              sum[b][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(now.x[t][2 * p + h], now.w[b][2 * p + h], sum[b][t], 0, 0, 0);
-      }
-      now = next;
+      for (int b = 0; b < RT; ++b)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) sum[b][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(x[t], w[b], sum[b][t], 0, 0, 0);
     }
+  };
+  for (int s = 0; s < F::STAGES - 1 && s < steps; ++s) copy(s, s);
+  int stage = 0;
+  for (int step = 0; step < steps; ++step) {
+    // This step's copies are behind all but those of the STAGES - 2 steps after it, and every wave is done with the
+    // stage before, which the next copies fill.
+    if (step + F::STAGES - 2 < steps)
+      arrived<(F::STAGES - 2) * F::COPIES>();
+    else
+      arrived<0>();
+    const int before = stage ? stage - 1 : F::STAGES - 1;
+    if (step + F::STAGES - 1 < steps) copy(step + F::STAGES - 1, before);
+    if (line_of(step) < lines) multiply(stage);
+    stage = stage + 1 < F::STAGES ? stage + 1 : 0;
   }
-  // A lane has weight row r16 and rows 4 quarter .. of x.  The first of a tile's waves finishes what all have.
-  i32x4* joined = reinterpret_cast<i32x4*>(lds);
-  if (split > 1) {
+  // A lane has weight row r16 and rows 4 quarter .. of x.  The first of the waves that share columns finishes what all have.
+  if (F::WK > 1) {
+    __syncthreads();
+    i32x4* joined = reinterpret_cast<i32x4*>(lds);
     if (part) {
 #pragma unroll
       for (int b = 0; b < RT; ++b)
@@ -101,17 +150,18 @@ __global__ __launch_bounds__(512) void q8_few_kernel(const Q8Args a) {
     }
     __syncthreads();
     if (part) return;
-    for (int p = 1; p < split; ++p)
+#pragma unroll
+    for (int p = 1; p < F::WK; ++p)
 #pragma unroll
       for (int b = 0; b < RT; ++b)
 #pragma unroll
-        for (int t = 0; t < NT; ++t) sum[b][t] += joined[(((wave + p) * RT + b) * NT + t) * 64 + lane];
+        for (int t = 0; t < NT; ++t) sum[b][t] += joined[(((wave + p * WW) * RT + b) * NT + t) * 64 + lane];
   }
   const float* scales = a.scales + (int64_t)expert * a.M;
 #pragma unroll
   for (int b = 0; b < RT; ++b) {
-    if (pair == 2 && b) continue;
-    const int64_t m = m0 + 16 * b + r16;
+    if (pair == 2 && b % 2) continue;
+    const int64_t m = m0 + (pair == 2 ? b / 2 : b) * 16 + r16;
     if (m >= a.out_rows) continue;
     const float ws = scales[m], wu = pair == 2 ? scales[a.out_rows + m] : 0.f;
 #pragma unroll
@@ -123,7 +173,7 @@ __global__ __launch_bounds__(512) void q8_few_kernel(const Q8Args a) {
         const float xs = a.xs[q8_x_row(a, n)];
         float v = (float)sum[b][t][i] * (xs * ws);
         if (RT > 1 && pair == 2) {
-          const float up = (float)sum[RT > 1 ? 1 : 0][t][i] * (xs * wu);
+          const float up = (float)sum[b + 1 < RT ? b + 1 : b][t][i] * (xs * wu);
           v = (a.y_type == EBAG_F32 ? silu<true>(v) : silu<false>(v)) * up;
         }
         q8_store(a, n, m, v);
@@ -131,16 +181,30 @@ __global__ __launch_bounds__(512) void q8_few_kernel(const Q8Args a) {
   }
 }
 
+template <int RT, int NT, int WW, int WAVES>
+void launch(const Q8Args& a, unsigned grid, hipStream_t stream) {
+  hipLaunchKernelGGL((q8_few_kernel<RT, NT, WW, WAVES>), dim3(grid), dim3(64 * WAVES), (Few<RT, NT, WW, WAVES>::LDS), stream, a);
+}
+
 template <int RT>
-void (*pick(int x_tiles))(const Q8Args) {
-  return x_tiles == 1 ? q8_few_kernel<RT, 1> : x_tiles == 2 ? q8_few_kernel<RT, 2> : q8_few_kernel<RT, 4>;
+void launch(const Q8Args& a, int x_tiles, int waves, unsigned grid, hipStream_t stream) {
+  switch (x_tiles * 16 + waves) {
+    case 16 + 1: return launch<RT, 1, 1, 4>(a, grid, stream);
+    case 16 + 2: return launch<RT, 1, 2, 4>(a, grid, stream);
+    case 32 + 1: return launch<RT, 2, 1, 4>(a, grid, stream);
+    case 32 + 2: return launch<RT, 2, 2, 4>(a, grid, stream);
+    case 32 + 4: return launch<RT, 2, 4, 4>(a, grid, stream);
+    case 64 + 1: return launch<RT, 4, 1, 4>(a, grid, stream);
+    case 64 + 2: return launch<RT, 4, 2, 4>(a, grid, stream);
+    case 64 + 4: return launch<RT, 4, 4, 4>(a, grid, stream);
+    default: return launch<RT, 4, 8, 8>(a, grid, stream);
+  }
 }
 
 }  // namespace
 
-void launch_q8_few(const Q8Args& a, int tiles, int x_tiles, unsigned grid, int threads, hipStream_t stream) {
-  const size_t lds = a.split > 1 ? (size_t)threads * tiles * x_tiles * 16 : 0;
-  hipLaunchKernelGGL(tiles == 1 ? pick<1>(x_tiles) : pick<2>(x_tiles), dim3(grid), dim3(threads), lds, stream, a);
+void launch_q8_few(const Q8Args& a, int tiles, int x_tiles, int waves, unsigned grid, hipStream_t stream) {
+  tiles == 1 ? launch<1>(a, x_tiles, waves, grid, stream) : launch<2>(a, x_tiles, waves, grid, stream);
 }
 
 }  // namespace ebag
