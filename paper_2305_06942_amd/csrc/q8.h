@@ -5,6 +5,7 @@
 #include <stdint.h>
 
 #include "common.h"
+#include "lanes.h"
 #include "products.h"
 #include "vec16.h"
 
@@ -36,6 +37,10 @@ struct Q8Args {
   int32_t experts;
   int32_t glu;
   int32_t y_type;
+  const char* x;            // rows to be rounded by the product itself (kQ8Own at most, launch_q8_own alone)
+  int64_t ldx;              // bytes
+  int32_t x_type;
+  int32_t K;
   Divisor by_choices;
   Divisor by_tiles;         // workgroups that share the rows of x, each with its rows of weights
   // The matrix-product kernel.
@@ -58,6 +63,71 @@ __device__ __forceinline__ void q8_store(const Q8Args& a, uint32_t n, int64_t m,
     reinterpret_cast<__bf16*>(p)[m] = Type<2>::narrow(v);
 }
 
+// The largest over the 64 lanes, in each of them; of numbers without a sign, as whole numbers keep the order of
+// floats and put NaN above infinity.
+__device__ __forceinline__ uint32_t q8_larger(uint32_t a, uint32_t b) { return a > b ? a : b; }
+template <int CTRL>
+__device__ __forceinline__ uint32_t q8_larger_dpp(uint32_t v) {
+  return q8_larger(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ uint32_t q8_largest(uint32_t v) {
+  v = q8_larger_dpp<0xB1>(v);
+  v = q8_larger_dpp<0x4E>(v);
+  v = q8_larger_dpp<0x141>(v);
+  v = q8_larger_dpp<0x140>(v);
+  const u32x2 s = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = q8_larger(s[0], s[1]);
+  const u32x2 t = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return q8_larger(t[0], t[1]);
+}
+
+// Eight neighbouring elements in fp32, zeros behind the row's end.
+template <int DT>
+__device__ __forceinline__ void q8_load8(const char* row, int at, int K, float* f) {
+  typedef Type<DT> T;
+  typedef typename T::elt elt;
+  if (at + 8 <= K) {
+#pragma unroll
+    for (int v = 0; v < 8 / T::N; ++v) T::widen(load16(row + (int64_t)at * sizeof(elt) + 16 * v), f + v * T::N);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = at + i < K ? T::widen(reinterpret_cast<const elt*>(row)[at + i]) : 0.f;
+  }
+}
+
+// The whole number nearest to x / scale, halves to even: what the product with the reciprocal gives is at most one
+// off, and x less that many scales, exact up to its sign and its order with scale / 2, says which way.
+__device__ __forceinline__ float q8_scale(uint32_t top) {  // of a row whose largest size has these bits
+  return top >= 0x7f800000u ? __builtin_nanf("") : __uint_as_float(top) / 127.f;
+}
+
+struct Q8Rounder {
+  float scale, inv, half, factor;
+  bool any;
+  __device__ __forceinline__ Q8Rounder(float s) {
+    // Scales so small that their reciprocal would not be a number, or their half not exact, are taken 2^64 times.
+    factor = s < 0x1p-60f ? 0x1p64f : 1.f;
+    scale = s * factor;
+    any = s > 0.f;  // not NaN
+    inv = any ? 1.f / scale : 0.f;
+    half = 0.5f * scale;
+  }
+  __device__ __forceinline__ int code(float x) const {
+    x *= factor;
+    float q = rintf(x * inv);
+    const float left = fmaf(-q, scale, x), size = fabsf(left);
+    if (size > half || (size == half && ((int)q & 1))) q += left > 0.f ? 1.f : -1.f;
+    return any ? (int)fminf(fmaxf(q, -127.f), 127.f) : 0;
+  }
+};
+
+__device__ __forceinline__ void q8_store8(int8_t* to, const Q8Rounder& r, const float* f) {
+  uint32_t w[2] = {0, 0};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) w[i / 4] |= ((uint32_t)r.code(f[i]) & 0xffu) << (8 * (i % 4));
+  *reinterpret_cast<uint2*>(to) = uint2{w[0], w[1]};
+}
+
 // Rows of weights and rows of x of a workgroup of the matrix-product kernel.
 enum Q8Tile { Q8_256x64, Q8_512x128, Q8_256x256 };
 constexpr int q8_tile_w(Q8Tile t) { return t == Q8_512x128 ? 512 : 256; }
@@ -65,6 +135,10 @@ constexpr int q8_tile_x(Q8Tile t) { return t == Q8_256x64 ? 64 : t == Q8_512x128
 
 // tiles: of 16 rows of weights of a wave; x_tiles: of 16 rows of x; waves: of four, that have different rows of weights.
 void launch_q8_few(const Q8Args& a, int tiles, int x_tiles, int waves, unsigned grid, hipStream_t stream);
+// The same for at most kQ8Own rows of x of any type, of whole 16-byte vectors on 16-byte boundaries.
+constexpr int kQ8Own = 2;
+bool q8_own_fits(const Q8Args& a);
+void launch_q8_own(const Q8Args& a, int tiles, int waves, unsigned grid, hipStream_t stream);
 void launch_q8_tile(const Q8Args& a, Q8Tile kind, unsigned grid, hipStream_t stream);
 
 }  // namespace ebag

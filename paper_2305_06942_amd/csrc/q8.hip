@@ -7,7 +7,6 @@
 
 #include "ebag_a2a.h"
 #include "gemv_ar.h"
-#include "lanes.h"
 #include "q8.h"
 
 using namespace ebag;
@@ -29,67 +28,6 @@ struct RoundArgs {
   int32_t K;
   int32_t units;    // of 8 elements, the last one short or empty: pitch / 8
 };
-
-// The largest over the 64 lanes, in each of them; of numbers without a sign, as whole numbers keep the order of
-// floats and put NaN above infinity.
-__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return a > b ? a : b; }
-template <int CTRL>
-__device__ __forceinline__ uint32_t larger_dpp(uint32_t v) {
-  return larger(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true));
-}
-__device__ __forceinline__ uint32_t largest(uint32_t v) {
-  v = larger_dpp<0xB1>(v);
-  v = larger_dpp<0x4E>(v);
-  v = larger_dpp<0x141>(v);
-  v = larger_dpp<0x140>(v);
-  const u32x2 s = __builtin_amdgcn_permlane16_swap(v, v, false, false);
-  v = larger(s[0], s[1]);
-  const u32x2 t = __builtin_amdgcn_permlane32_swap(v, v, false, false);
-  return larger(t[0], t[1]);
-}
-
-// Eight neighbouring elements in fp32, zeros behind the row's end.
-template <int DT>
-__device__ __forceinline__ void load8(const char* row, int at, int K, float* f) {
-  typedef Type<DT> T;
-  typedef typename T::elt elt;
-  if (at + 8 <= K) {
-#pragma unroll
-    for (int v = 0; v < 8 / T::N; ++v) T::widen(load16(row + (int64_t)at * sizeof(elt) + 16 * v), f + v * T::N);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = at + i < K ? T::widen(reinterpret_cast<const elt*>(row)[at + i]) : 0.f;
-  }
-}
-
-// The whole number nearest to x / scale, halves to even: what the product with the reciprocal gives is at most one
-// off, and x less that many scales, exact up to its sign and its order with scale / 2, says which way.
-struct Rounder {
-  float scale, inv, half, factor;
-  bool any;
-  __device__ __forceinline__ Rounder(float s) {
-    // Scales so small that their reciprocal would not be a number, or their half not exact, are taken 2^64 times.
-    factor = s < 0x1p-60f ? 0x1p64f : 1.f;
-    scale = s * factor;
-    any = s > 0.f;  // not NaN
-    inv = any ? 1.f / scale : 0.f;
-    half = 0.5f * scale;
-  }
-  __device__ __forceinline__ int code(float x) const {
-    x *= factor;
-    float q = rintf(x * inv);
-    const float left = fmaf(-q, scale, x), size = fabsf(left);
-    if (size > half || (size == half && ((int)q & 1))) q += left > 0.f ? 1.f : -1.f;
-    return any ? (int)fminf(fmaxf(q, -127.f), 127.f) : 0;
-  }
-};
-
-__device__ __forceinline__ void store8(int8_t* to, const Rounder& r, const float* f) {
-  uint32_t w[2] = {0, 0};
-#pragma unroll
-  for (int i = 0; i < 8; ++i) w[i / 4] |= ((uint32_t)r.code(f[i]) & 0xffu) << (8 * (i % 4));
-  *reinterpret_cast<uint2*>(to) = uint2{w[0], w[1]};
-}
 
 // WAVE: a wave to a row, otherwise a workgroup.  Up to 32 elements of a lane stay in registers between
 // the largest and the codes; longer rows are read again.
@@ -114,34 +52,34 @@ __global__ __launch_bounds__(kRoundThreads) void q8_round_kernel(const RoundArgs
   for (int u = 0; u < kHeld; ++u) {
     const int unit = u * lanes + lane;
     if (unit < a.units) {
-      load8<DT>(x, unit * 8, a.K, held[u]);
+      q8_load8<DT>(x, unit * 8, a.K, held[u]);
       look(held[u]);
     }
   }
   for (int unit = kHeld * lanes + lane; unit < a.units; unit += lanes) {
     float f[8];
-    load8<DT>(x, unit * 8, a.K, f);
+    q8_load8<DT>(x, unit * 8, a.K, f);
     look(f);
   }
-  top = largest(top);
+  top = q8_largest(top);
   if (!WAVE) {
     if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < kRoundThreads / 64; ++w) top = top > tops[w] ? top : tops[w];
   }
-  const float scale = top >= 0x7f800000u ? __builtin_nanf("") : __uint_as_float(top) / 127.f;
+  const float scale = q8_scale(top);
   if (lane == 0) a.scales[row] = scale;
-  const Rounder r(scale);
+  const Q8Rounder r(scale);
 #pragma unroll
   for (int u = 0; u < kHeld; ++u) {
     const int unit = u * lanes + lane;
-    if (unit < a.units) store8(codes + unit * 8, r, held[u]);
+    if (unit < a.units) q8_store8(codes + unit * 8, r, held[u]);
   }
   for (int unit = kHeld * lanes + lane; unit < a.units; unit += lanes) {
     float f[8];
-    load8<DT>(x, unit * 8, a.K, f);
-    store8(codes + unit * 8, r, f);
+    q8_load8<DT>(x, unit * 8, a.K, f);
+    q8_store8(codes + unit * 8, r, f);
   }
 }
 
@@ -214,6 +152,10 @@ int fill_args(const gemv_ar_q8_plan* h, const int8_t* codes, const float* scales
   *a = Q8Args{};
   a->codes = codes;
   a->scales = scales;
+  a->x = static_cast<const char*>(x);
+  a->ldx = ldx * elt_of(h->dtype);
+  a->x_type = h->dtype;
+  a->K = (int32_t)h->K;
   a->xq = xq;
   a->xs = xs;
   a->y = static_cast<char*>(y);
@@ -245,7 +187,10 @@ int launch_few(Q8Args a, int x_tiles, hipStream_t stream) {
   const int64_t grid_tiles = (wave_tiles + waves - 1) / waves;
   if (grid_tiles * slots > INT_MAX) return fail(EBAG_EUNSUPPORTED, "too many tiles for one launch");
   a.by_tiles = make_divisor(grid_tiles);
-  launch_q8_few(a, a.glu ? 2 : 1, x_tiles, waves, (unsigned)(grid_tiles * slots), stream);
+  if (a.x)
+    launch_q8_own(a, a.glu ? 2 : 1, waves, (unsigned)grid_tiles, stream);
+  else
+    launch_q8_few(a, a.glu ? 2 : 1, x_tiles, waves, (unsigned)(grid_tiles * slots), stream);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? EBAG_OK : hipf(e, "launch the product in 8 bits");
 }
@@ -329,8 +274,11 @@ int gemv_ar_q8_forward(gemv_ar_q8_t h, const int8_t* codes, const float* scales,
   if (!rows) return EBAG_OK;
   Q8Args a;
   if (int rc = fill_args(h, codes, scales, x, ldx, rows, xq, xs, rows, y, ldy, y_dtype, &a)) return rc;
-  if (x)
-    if (int rc = launch_round(h, x, ldx, rows, xq, xs, stream)) return rc;
+  if (!q8_own_fits(a)) {
+    if (x)
+      if (int rc = launch_round(h, x, ldx, rows, xq, xs, stream)) return rc;
+    a.x = nullptr;
+  }
   return launch(a, stream);
 }
 
@@ -349,6 +297,7 @@ int gemv_ar_q8_experts(gemv_ar_q8_t h, const int8_t* codes, const float* scales,
   a.offsets = offsets;
   a.src = src;
   a.by_choices = make_divisor(src ? choices : 1);
+  a.x = nullptr;
   if (x)
     if (int rc = launch_round(h, x, ldx, x_rows, xq, xs, stream)) return rc;
   return launch(a, stream);

@@ -26,15 +26,15 @@ __device__ __forceinline__ void arrived() {
 // and the up rows that go with them), and WK = WAVES / WW share the columns, each a part of whole lines of 128.  All of
 // them have the same NT tiles of 16 rows of x.  A line of each row goes through LDS, in a ring of STAGES of them.
 // Sums are whole numbers, so the order in which the parts of the columns are joined does not matter.
-template <int RT, int NT, int WW, int WAVES>
+template <int RT, int NT, int WW, int WAVES, bool OWN>
 struct Few {
   static constexpr int WK = WAVES / WW;
-  static constexpr int W_ROWS = 16 * RT * WW, X_ROWS = 16 * NT, ROWS = W_ROWS + X_ROWS;  // of a part of the columns
+  static constexpr int W_ROWS = 16 * RT * WW, X_ROWS = OWN ? 0 : 16 * NT, ROWS = W_ROWS + X_ROWS;  // of a part of the columns
   static constexpr int STAGE = WK * ROWS * (int)kQ8Line;
   static constexpr int X_COPIES = X_ROWS / 8 / WW, COPIES = 2 * RT + X_COPIES;           // of a wave, eight rows each
   static_assert(X_COPIES * 8 * WW == X_ROWS, "");
   // Three workgroups on a CU, or two, or one.
-  static constexpr int RING = kCuLds / (STAGE * 9 <= kCuLds ? 3 : STAGE * 6 <= kCuLds ? 2 : 1);
+  static constexpr int RING = kCuLds / (STAGE * 9 <= kCuLds ? 3 : STAGE * 6 <= kCuLds ? 2 : 1) - (OWN ? 4096 : 0);
   static constexpr int FIT = RING / STAGE, MOST = 62 / COPIES + 2;
   static constexpr int STAGES = FIT < MOST ? FIT : MOST;
   static_assert(STAGES >= 3, "");
@@ -42,9 +42,41 @@ struct Few {
   static constexpr int LDS = STAGES * STAGE > JOIN ? STAGES * STAGE : JOIN;
 };
 
-template <int RT, int NT, int WW, int WAVES>
+template <int DT>
+__device__ __forceinline__ void round_rows(const Q8Args& a, const char* raw, int raw_pitch, int8_t* codes, float* scales, uint32_t* tops) {
+  const int waves = blockDim.x >> 6, wave = threadIdx.x >> 6, units = (int)(a.pitch / 8);
+  for (int r = 0; r < (int)a.rows; ++r) {
+    uint32_t top = 0;
+    for (int u = threadIdx.x; u < units; u += blockDim.x) {
+      float f[8];
+      q8_load8<DT>(raw + r * raw_pitch, u * 8, a.K, f);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top = q8_larger(top, __float_as_uint(f[i]) & 0x7fffffffu);
+    }
+    top = q8_largest(top);
+    if ((threadIdx.x & 63) == 0) tops[r * waves + wave] = top;
+  }
+  __syncthreads();
+  for (int r = 0; r < (int)a.rows; ++r) {
+    uint32_t top = 0;
+    for (int w = 0; w < waves; ++w) top = q8_larger(top, tops[r * waves + w]);
+    const float scale = q8_scale(top);
+    if (threadIdx.x == 0) scales[r] = scale;
+    const Q8Rounder rounder(scale);
+    for (int u = threadIdx.x; u < units; u += blockDim.x) {
+      float f[8];
+      q8_load8<DT>(raw + r * raw_pitch, u * 8, a.K, f);
+      q8_store8(codes + r * a.pitch + u * 8, rounder, f);
+    }
+  }
+  __syncthreads();
+}
+
+// OWN: the rows of x, two at most, are rounded here, by every workgroup for itself, while the first weights
+// are on their way: a launch less.
+template <int RT, int NT, int WW, int WAVES, bool OWN>
 __global__ __launch_bounds__(64 * WAVES) void q8_few_kernel(const Q8Args a) {
-  typedef Few<RT, NT, WW, WAVES> F;
+  typedef Few<RT, NT, WW, WAVES, OWN> F;
   extern __shared__ __attribute__((aligned(16))) char lds[];
   const int lane = threadIdx.x & 63, r16 = lane & 15, quarter = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave_w = wave % WW, part = wave / WW;
@@ -91,6 +123,19 @@ __global__ __launch_bounds__(64 * WAVES) void q8_few_kernel(const Q8Args a) {
     from[i] += ((lane & 7) ^ (row >> 1 & 7)) * 16;
     to[i] = lds0 + __builtin_amdgcn_readfirstlane(row - row8) * (int)kQ8Line;
   }
+  // OWN: behind the ring the rows' codes, then the rows as they are, in whole KiB, then their scales and the waves' largest.
+  char* codes = lds + F::LDS;
+  const int raw_bytes = OWN ? a.K * (a.x_type == EBAG_F32 ? 4 : 2) : 0, raw_pitch = (raw_bytes + 1023) / 1024 * 1024;
+  char* raw = codes + (OWN ? a.rows * a.pitch : 0);
+  float* own_scales = reinterpret_cast<float*>(raw + (OWN ? (int)a.rows : 0) * raw_pitch);
+  if (OWN) {
+    const int chunks = raw_pitch / 1024;
+    for (int i = wave; i < (int)a.rows * chunks; i += WAVES) {
+      const int r = i / chunks, at = (i - r * chunks) * 1024 + lane * 16;
+      copy_to_lds((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)raw + i * 1024,
+                  reinterpret_cast<const int8_t*>(a.x + r * a.ldx + (at < raw_bytes ? at : raw_bytes - 16)));
+    }
+  }
   const int lines = (int)(a.pitch / kQ8Line), steps = (lines + F::WK - 1) / F::WK, line0 = part * steps;
   // Not every workgroup begins with its first line: rows of a power of two bytes would have all of them ask the same
   // memory channels at a time (16 rows x 65536 x 8192: 117 us, like this 92; each eight neighbours, on an XCD each, alike).
@@ -108,7 +153,8 @@ __global__ __launch_bounds__(64 * WAVES) void q8_few_kernel(const Q8Args a) {
   for (int b = 0; b < RT; ++b)
 #pragma unroll
     for (int t = 0; t < NT; ++t) sum[b][t] = i32x4{0, 0, 0, 0};
-  auto multiply = [&](int stage) __attribute__((always_inline)) {
+  const char* own_x = codes + (r16 < (int)a.rows ? r16 : 0) * a.pitch + quarter * 16;
+  auto multiply = [&](int stage, int line) __attribute__((always_inline)) {
     const char* rows = mine + stage * F::STAGE;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -117,7 +163,8 @@ __global__ __launch_bounds__(64 * WAVES) void q8_few_kernel(const Q8Args a) {
 #pragma unroll
       for (int b = 0; b < RT; ++b) w[b] = *reinterpret_cast<const i32x4*>(rows + (wave_w * RT + b) * (16 * (int)kQ8Line) + piece);
 #pragma unroll
-      for (int t = 0; t < NT; ++t) x[t] = *reinterpret_cast<const i32x4*>(rows + (F::W_ROWS + 16 * t) * (int)kQ8Line + piece);
+      for (int t = 0; t < NT; ++t)
+        x[t] = *reinterpret_cast<const i32x4*>(OWN ? own_x + line * (int)kQ8Line + h * 64 : rows + (F::W_ROWS + 16 * t) * (int)kQ8Line + piece);
 #pragma unroll
       for (int b = 0; b < RT; ++b)
 #pragma unroll
@@ -125,6 +172,20 @@ __global__ __launch_bounds__(64 * WAVES) void q8_few_kernel(const Q8Args a) {
     }
   };
   for (int s = 0; s < F::STAGES - 1 && s < steps; ++s) copy(s, s);
+  if (OWN) {
+    if (steps >= F::STAGES - 1)
+      arrived<(F::STAGES - 1) * F::COPIES>();
+    else
+      arrived<0>();
+    uint32_t* tops = reinterpret_cast<uint32_t*>(own_scales + kQ8Own);
+    int8_t* to_codes = reinterpret_cast<int8_t*>(codes);
+    if (a.x_type == EBAG_F32)
+      round_rows<0>(a, raw, raw_pitch, to_codes, own_scales, tops);
+    else if (a.x_type == EBAG_F16)
+      round_rows<1>(a, raw, raw_pitch, to_codes, own_scales, tops);
+    else
+      round_rows<2>(a, raw, raw_pitch, to_codes, own_scales, tops);
+  }
   int stage = 0;
   for (int step = 0; step < steps; ++step) {
     // This step's copies are behind all but those of the STAGES - 2 steps after it, and every wave is done with the
@@ -135,7 +196,7 @@ __global__ __launch_bounds__(64 * WAVES) void q8_few_kernel(const Q8Args a) {
       arrived<0>();
     const int before = stage ? stage - 1 : F::STAGES - 1;
     if (step + F::STAGES - 1 < steps) copy(step + F::STAGES - 1, before);
-    if (line_of(step) < lines) multiply(stage);
+    if (line_of(step) < lines) multiply(stage, line_of(step));
     stage = stage + 1 < F::STAGES ? stage + 1 : 0;
   }
   // A lane has weight row r16 and rows 4 quarter .. of x.  The first of the waves that share columns finishes what all have.
@@ -170,7 +231,7 @@ __global__ __launch_bounds__(64 * WAVES) void q8_few_kernel(const Q8Args a) {
       for (int i = 0; i < 4; ++i) {
         const uint32_t n = first + 16 * t + 4 * quarter + i;
         if (n >= end) continue;
-        const float xs = a.xs[q8_x_row(a, n)];
+        const float xs = OWN ? own_scales[n] : a.xs[q8_x_row(a, n)];
         float v = (float)sum[b][t][i] * (xs * ws);
         if (RT > 1 && pair == 2) {
           const float up = (float)sum[b + 1 < RT ? b + 1 : b][t][i] * (xs * wu);
@@ -183,7 +244,17 @@ __global__ __launch_bounds__(64 * WAVES) void q8_few_kernel(const Q8Args a) {
 
 template <int RT, int NT, int WW, int WAVES>
 void launch(const Q8Args& a, unsigned grid, hipStream_t stream) {
-  hipLaunchKernelGGL((q8_few_kernel<RT, NT, WW, WAVES>), dim3(grid), dim3(64 * WAVES), (Few<RT, NT, WW, WAVES>::LDS), stream, a);
+  hipLaunchKernelGGL((q8_few_kernel<RT, NT, WW, WAVES, false>), dim3(grid), dim3(64 * WAVES), (Few<RT, NT, WW, WAVES, false>::LDS), stream, a);
+}
+
+int own_bytes(const Q8Args& a) {  // of LDS, behind the ring
+  const int raw = a.K * (a.x_type == EBAG_F32 ? 4 : 2);
+  return (int)a.rows * ((int)a.pitch + (raw + 1023) / 1024 * 1024) + 4 * kQ8Own * (1 + 4);
+}
+
+template <int RT, int WW>
+void launch_own(const Q8Args& a, unsigned grid, hipStream_t stream) {
+  hipLaunchKernelGGL((q8_few_kernel<RT, 1, WW, 4, true>), dim3(grid), dim3(256), (Few<RT, 1, WW, 4, true>::LDS) + own_bytes(a), stream, a);
 }
 
 template <int RT>
@@ -202,6 +273,20 @@ void launch(const Q8Args& a, int x_tiles, int waves, unsigned grid, hipStream_t 
 }
 
 }  // namespace
+
+// Up to two thirds of a CU's LDS next to the ring, and x as copies take it.
+bool q8_own_fits(const Q8Args& a) {
+  const int elt = a.x_type == EBAG_F32 ? 4 : 2;
+  return a.x && a.rows <= kQ8Own && !a.offsets && (int64_t)a.K * elt % 16 == 0 && a.ldx % 16 == 0 &&
+         reinterpret_cast<uintptr_t>(a.x) % 16 == 0 && own_bytes(a) <= kCuLds * 2 / 3;
+}
+
+void launch_q8_own(const Q8Args& a, int tiles, int waves, unsigned grid, hipStream_t stream) {
+  if (tiles == 1)
+    waves == 1 ? launch_own<1, 1>(a, grid, stream) : launch_own<1, 2>(a, grid, stream);
+  else
+    waves == 1 ? launch_own<2, 1>(a, grid, stream) : launch_own<2, 2>(a, grid, stream);
+}
 
 void launch_q8_few(const Q8Args& a, int tiles, int x_tiles, int waves, unsigned grid, hipStream_t stream) {
   tiles == 1 ? launch<1>(a, x_tiles, waves, grid, stream) : launch<2>(a, x_tiles, waves, grid, stream);
