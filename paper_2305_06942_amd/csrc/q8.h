@@ -42,7 +42,10 @@ struct Q8Args {
   int32_t x_type;
   int32_t K;
   Divisor by_choices;
-  Divisor by_tiles;         // workgroups that share the rows of x, each with its rows of weights
+  Divisor by_tiles;         // workgroups that share the rows of x, each with its rows of weights: of the kernel for few
+                            // rows an eighth of them
+  uint32_t tiles;           // the kernel for few rows: all of them
+  Divisor by_group;         // and slots that have their turn with a workgroup's weights one after the other
   // The matrix-product kernel.
   uint32_t whole;           // workgroups in whole rounds of all XCDs
 };

@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <climits>
+#include <cmath>
 #include <new>
 
 #include "ebag_a2a.h"
@@ -182,15 +183,19 @@ int launch_few(Q8Args a, int x_tiles, hipStream_t stream) {
   const int64_t slots = a.offsets ? most_tiles(a.rows, a.experts, cols) : (a.rows + cols - 1) / cols;
   const int64_t wave_tiles = (a.out_rows + 15) / 16, used = a.offsets ? (a.rows + cols - 1) / cols : slots;
   const int most = x_tiles == 1 ? 2 : x_tiles == 2 ? 4 : 8;
-  int waves = 1;
+  int waves = x_tiles == 8 ? 4 : 1;
   while (waves < most && wave_tiles * used >= 200 * 2 * waves) waves *= 2;
-  const int64_t grid_tiles = (wave_tiles + waves - 1) / waves;
-  if (grid_tiles * slots > INT_MAX) return fail(EBAG_EUNSUPPORTED, "too many tiles for one launch");
-  a.by_tiles = make_divisor(grid_tiles);
+  const int64_t grid_tiles = (wave_tiles + waves - 1) / waves, eighths = (grid_tiles + 7) / 8;
+  const int64_t group = a.offsets ? (a.rows > (int64_t)cols * a.experts ? 4 : 1) : slots < 8 ? slots : 8, groups = (slots + group - 1) / group;
+  const int64_t grid = 8 * eighths * group * groups;
+  if (grid > INT_MAX) return fail(EBAG_EUNSUPPORTED, "too many tiles for one launch");
+  a.by_tiles = make_divisor(eighths);
+  a.tiles = (uint32_t)grid_tiles;
+  a.by_group = make_divisor(group);
   if (a.x)
-    launch_q8_own(a, a.glu ? 2 : 1, waves, (unsigned)grid_tiles, stream);
+    launch_q8_own(a, a.glu ? 2 : 1, waves, (unsigned)grid, stream);
   else
-    launch_q8_few(a, a.glu ? 2 : 1, x_tiles, waves, (unsigned)(grid_tiles * slots), stream);
+    launch_q8_few(a, a.glu ? 2 : 1, x_tiles, waves, (unsigned)grid, stream);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? EBAG_OK : hipf(e, "launch the product in 8 bits");
 }
@@ -208,12 +213,58 @@ int launch_tile(Q8Args a, Q8Tile kind, hipStream_t stream) {
   return e == hipSuccess ? EBAG_OK : hipf(e, "launch the product in 8 bits");
 }
 
+// Which kernel, by a model of measured times in us.  A kernel has `cols` rows of x and `rows` of weights to a workgroup.
+// `fix` is its beginning and end; K = 4096 (times K / 4096 for others) takes at least `least`, a workgroup's own time, and
+// otherwise `start` and `each` ns for every 16 x 16 sums, or `round` for every 256 workgroups of the largest tiles, one
+// to a CU.  Where the weights are more than the caches hold, memory's rate bounds all of them, `rate` in TB/s, at 1.5 times
+// the bytes with two tiles of x and so on in the kernel that streams (its tiles of x share weights in the L2 by half).
+//   bf16 x 4096 x 4096, in us by 16, 32, 64 and 128 rows of x in the streaming kernel, 256 x 64, 512 x 128 and 256 x 256:
+//     64 rows 9.8, 10.0, 11.5, 24, 20.6, 48, 46; 256 rows 25.5, 16.6, 18.8, 27, 21.1, 50, 48; 512 rows 47, 30, 20.2, 29, 21.8,
+//     50, 49; 2048 rows 164, 86, 53, 60, 41, 55, 51; 4096 rows 308, 155, 101, 114, 78, 64, 60
+//   128 rows x 65536 x 8192: 355, 207, 143, 120, 194, 213, 348
+//   gated experts of 2 x 1024 x 2048: 128 of them with 2 rows each 87, 90, 227, 139, 87, 99, 143; 64 with 32 rows each 91, 64,
+//     60, 92, 53, 59, 77; with 256 rows each 462, 243, 189, 174, 125, 131, 160
+struct Kernel {
+  int x_tiles;  // of 16 rows, in the streaming kernel; 0: the matrix-product kernel
+  Q8Tile tile;
+  double cols, rows, fix, least, start, each, round, rate;
+};
+constexpr Kernel kKernels[] = {
+    {1, Q8_256x64, 16, 16, 3, 1.5, 1.5, 5.2, 0, 5.6},   {2, Q8_256x64, 32, 16, 3, 4, 4, 2.75, 0, 5.6},
+    {4, Q8_256x64, 64, 16, 3, 7, 7, 1.3, 0, 5.6},       {8, Q8_256x64, 128, 16, 3, 21, 21, 1.0, 0, 4.5},
+    {0, Q8_256x64, 64, 256, 4, 16.5, 1, 1.17, 0, 5.4},  {0, Q8_512x128, 128, 512, 8, 40, 0, 0, 53, 2.5},
+    {0, Q8_256x256, 256, 256, 9, 37, 0, 0, 48, 1.5}};
+
+double time_of(const Kernel& k, const Q8Args& a) {
+  const double M = (double)a.M, scale = (double)a.pitch / 4096;
+  const double used = a.offsets ? (a.rows < (uint32_t)a.experts ? a.rows : a.experts) : 1;  // matrices with rows
+  const double per = (double)a.rows / used;
+  // Tiles of x: an expert's last one is half full on average.
+  double slots = a.offsets ? a.rows / k.cols + used / 2 : std::ceil(a.rows / k.cols);
+  slots = slots < used ? used : slots;
+  const double wgs = std::ceil(M / k.rows) * slots, sums = std::ceil(M / k.rows) * (k.rows / 16) * slots * (k.cols / 16);
+  double t = k.round ? std::ceil(wgs / 256) * k.round : k.start + sums * k.each * 1e-3;
+  t = k.fix + scale * (t < k.least ? k.least : t);
+  const double bytes = used * M * (double)a.pitch;
+  if (bytes > 128e6) {
+    double memory = bytes / (k.rate * 1e6);
+    if (k.x_tiles) memory *= (1 + 0.5 * (std::ceil(per / k.cols) - 1)) * (a.offsets && k.x_tiles > 1 ? 1.25 : 1);
+    // One workgroup on a CU, or two that share weights, have too few loads under way.
+    if (!k.x_tiles && !k.round && (wgs < 512 || (!a.offsets && per > k.cols))) memory *= 2;
+    if (memory > t) t = memory;
+  }
+  return t;
+}
+
 int launch(const Q8Args& a, hipStream_t stream) {
-  const double each = a.offsets ? (double)a.rows / a.experts : a.rows;  // rows of a matrix
-  if (each <= 16) return launch_few(a, 1, stream);
-  if (each <= 32) return launch_few(a, 2, stream);
-  if (each <= 64) return launch_few(a, 4, stream);
-  return launch_tile(a, each <= 128 ? Q8_256x64 : each <= 1024 ? Q8_512x128 : Q8_256x256, stream);
+  if (a.x) return launch_few(a, 1, stream);
+  const Kernel* best = nullptr;
+  double least = 0;
+  for (const Kernel& k : kKernels) {
+    const double t = time_of(k, a);
+    if (!best || t < least) best = &k, least = t;
+  }
+  return best->x_tiles ? launch_few(a, best->x_tiles, stream) : launch_tile(a, best->tile, stream);
 }
 
 }  // namespace

@@ -80,7 +80,12 @@ __global__ __launch_bounds__(64 * WAVES) void q8_few_kernel(const Q8Args a) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
   const int lane = threadIdx.x & 63, r16 = lane & 15, quarter = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave_w = wave % WW, part = wave / WW;
-  const uint32_t slot = divide_by(a.by_tiles, blockIdx.x), tile = blockIdx.x - slot * a.by_tiles.d;
+  // Neighbouring workgroups are on different XCDs: an XCD has every eighth tile of weights, for a group of slots one after
+  // the other, so that the second slot of one matrix finds them in the XCD's L2.
+  const uint32_t block = blockIdx.x >> 3, chunk = divide_by(a.by_group, block), in_group = block - chunk * a.by_group.d;
+  const uint32_t group = divide_by(a.by_tiles, chunk), eighth = chunk - group * a.by_tiles.d;
+  const uint32_t slot = group * a.by_group.d + in_group, tile = eighth * 8 + (blockIdx.x & 7);
+  if (tile >= a.tiles) return;
   int expert;
   uint32_t first, end;
   if (!find_tile(a, slot, 16 * NT, &expert, &first, &end)) return;
@@ -138,8 +143,8 @@ __global__ __launch_bounds__(64 * WAVES) void q8_few_kernel(const Q8Args a) {
   }
   const int lines = (int)(a.pitch / kQ8Line), steps = (lines + F::WK - 1) / F::WK, line0 = part * steps;
   // Not every workgroup begins with its first line: rows of a power of two bytes would have all of them ask the same
-  // memory channels at a time (16 rows x 65536 x 8192: 117 us, like this 92; each eight neighbours, on an XCD each, alike).
-  const int turn0 = (int)((blockIdx.x >> 3) % (uint32_t)steps);
+  // memory channels at a time (16 rows x 65536 x 8192: 117 us, like this 92; each eight neighbours, on an XCD each, alike, and the slots of a group).
+  const int turn0 = (int)(chunk % (uint32_t)steps);
   auto line_of = [&](int step) { return line0 + (step + turn0 < steps ? step + turn0 : step + turn0 - steps); };
   auto copy = [&](int step, int stage) __attribute__((always_inline)) {
     const int at = line_of(step), line = at < lines ? at : lines - 1;  // one again where there is none
@@ -268,7 +273,9 @@ void launch(const Q8Args& a, int x_tiles, int waves, unsigned grid, hipStream_t 
     case 64 + 1: return launch<RT, 4, 1, 4>(a, grid, stream);
     case 64 + 2: return launch<RT, 4, 2, 4>(a, grid, stream);
     case 64 + 4: return launch<RT, 4, 4, 4>(a, grid, stream);
-    default: return launch<RT, 4, 8, 8>(a, grid, stream);
+    case 64 + 8: return launch<RT, 4, 8, 8>(a, grid, stream);
+    case 128 + 4: return launch<RT, 8, 4, 4>(a, grid, stream);
+    default: return launch<RT, 8, 8, 8>(a, grid, stream);
   }
 }
 

@@ -165,8 +165,14 @@ FORWARD = [  # rows, M, K, glu, step, shift
     (1, 1, 1, 0, 0, 0), (1, 2, 3, 1, 1, 1), (1, 16, 128, 0, 0, 0), (2, 17, 129, 0, 3, 1), (4, 64, 1000, 1, 0, 0), (1, 513, 4096, 0, 0, 0),
     (12, 301, 5001, 0, 1, 3), (16, 34, 640, 1, 0, 0), (17, 100, 256, 0, 0, 0), (31, 70, 384, 1, 5, 1), (33, 48, 2100, 0, 0, 0), (64, 130, 300, 1, 0, 0),
     (1, 70000, 200, 0, 0, 0), (3, 66000, 130, 1, 0, 0), (64, 5000, 130, 0, 0, 0),
+    # Few rows: one row and two on 16-byte boundaries (rounded by the product) and off them, in both types of tiles; waves that
+    # share x by 2, 4 and 8; two, three and more tiles of x that share weights.
+    (1, 4096, 1024, 0, 0, 0), (2, 300, 512, 1, 8, 8), (2, 7000, 136, 0, 16, 0), (2, 300, 512, 1, 4, 0), (1, 13000, 64, 1, 0, 0), (2, 48, 12288, 0, 0, 0),
+    (16, 13001, 140, 0, 0, 0), (32, 13000, 130, 0, 0, 1), (32, 26000, 130, 1, 0, 0), (20, 3300, 2000, 0, 0, 0), (64, 26001, 140, 0, 1, 0),
+    (64, 52000, 130, 1, 0, 0), (50, 7000, 140, 0, 0, 0), (40, 500, 3000, 1, 0, 0), (96, 2000, 520, 0, 0, 0), (150, 400, 700, 1, 0, 0),
     (65, 5, 100, 0, 0, 0), (65, 256, 128, 0, 0, 0), (100, 258, 1000, 1, 2, 1), (129, 300, 513, 0, 0, 0), (200, 1030, 260, 1, 0, 0),
-    (257, 255, 129, 0, 1, 1), (700, 514, 384, 1, 0, 0), (1025, 700, 640, 0, 0, 0), (1300, 1400, 200, 1, 0, 3), (3000, 40, 128, 0, 0, 0)]
+    (257, 255, 129, 0, 1, 1), (700, 514, 384, 1, 0, 0), (1025, 700, 640, 0, 0, 0), (1300, 1400, 200, 1, 0, 3), (3000, 40, 128, 0, 0, 0),
+    (2000, 6200, 129, 0, 0, 0), (6100, 2050, 300, 1, 1, 1), (4100, 4104, 257, 0, 0, 0), (1500, 2100, 1100, 0, 0, 0)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -224,7 +230,8 @@ def _offsets(rng, rows, E, dropped, empty):
 EXPERTS = [  # rows, E, M, K, glu, k, dropped, empty
     (1, 1, 16, 128, 0, 1, 0, 0), (1, 9, 5, 100, 0, 1, 1, 0), (8, 70, 34, 129, 1, 2, 1, 0.5), (64, 130, 20, 256, 0, 4, 5, 0.3), (300, 60, 70, 250, 1, 3, 17, 0),
     (256, 8, 130, 384, 0, 8, 0, 0.3), (500, 8, 66, 130, 1, 4, 33, 0), (900, 9, 300, 200, 0, 3, 100, 0.2), (2000, 12, 514, 128, 1, 8, 0, 0),
-    (2600, 2, 260, 256, 0, 2, 7, 0), (1200, 512, 8, 64, 0, 1, 3, 0.5), (6000, 4, 130, 130, 1, 6, 1000, 0.3)]
+    (2600, 2, 260, 256, 0, 2, 7, 0), (1200, 512, 8, 64, 0, 1, 3, 0.5), (6000, 4, 130, 130, 1, 6, 1000, 0.3),
+    (40, 3, 3000, 260, 0, 2, 0, 0), (70, 40, 700, 300, 1, 2, 2, 0.2), (5000, 6, 2100, 260, 1, 4, 50, 0.2), (400, 3, 4100, 130, 0, 1, 0, 0)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
