@@ -460,80 +460,108 @@ __global__ __launch_bounds__(256) void choose_join_kernel(const ChooseArgs a, in
 // softmax: dlogits[e] = p_e (a_e - <p, a> + q), and of the weights w with gradients d,
 // in the chosen places w_j (d_j - <w, d>) where they are normalised, otherwise w_j d_j,
 // and -p_e <w, d> everywhere.  The softmax is found anew: its row is read anyway.
+//
+// A chosen expert's logit is looked up in LDS, where the row lies until its places are
+// needed for the chosen experts' part of the gradient.  Bound by its chain of steps, not by bytes.
 template <int V, int L>
 __global__ __launch_bounds__(256) void choose_backward_kernel(const ChooseArgs a) {
-  __shared__ float places[256 / L][V * L];  // of the chosen places, logit (u, lane, c) at ((u * 4 + c) * L + lane)
+  __shared__ float places[256 / L][V * L];  // logit (u, lane, c) at ((u * 4 + c) * L + lane)
   const int lane = threadIdx.x % L, own = threadIdx.x / L;
   const int E = a.E, k = a.k;
-  float* direct = places[own];
+  float* place = places[own];
+  auto place_of = [&](int id) { return ((id >> 2) / L * 4 + (id & 3)) * L + (id >> 2) % L; };
   const int64_t n = (int64_t)blockIdx.x * (256 / L) + own;
   const bool here = n < a.tokens;
   const bool live = here && (!a.live || a.live[n]);
+  const bool weighed = a.dweights != nullptr;
+  // A lane's first choice stays in registers; further ones, where there are more than L, are read again.
+  auto number = [&](int j) {
+    const int id = live && j < k ? a.ids[n * k + j] : -1;
+    return (uint32_t)id < (uint32_t)E ? id : -1;
+  };
+  const int id0 = weighed ? number(lane) : -1;
+  const float d0 = id0 >= 0 ? a.dweights[n * k + lane] : 0.f;
   const char* row = a.logits + n * a.ld;
   float x[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) x[i] = -__builtin_inff();
   if (live) load_logits<V, L>(a.dtype, E, row, lane, x);
+  float pull[V];
+  float tokens = 0.f, balance = 0.f, squares = 0.f;
+  if (a.dlosses) {
+    tokens = (float)a.counts[E];
+    balance = a.dlosses[0];
+    squares = a.dlosses[1];
 #pragma unroll
-  for (int i = 0; i < V; ++i) direct[i * L + lane] = 0.f;
+    for (int i = 0; i < V; ++i) {
+      const int e = (i / 4 * L + lane) * 4 + i % 4;
+      pull[i] = (float)a.counts[e < E ? e : E - 1];
+    }
+  }
+  float l0 = 0.f;
+  if (weighed) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) place[i * L + lane] = x[i];
+    __builtin_amdgcn_wave_barrier();
+    l0 = id0 >= 0 ? place[place_of(id0)] : -__builtin_inff();
+  }
   const float top = top_of<V, L>(x);
   const bool counted = top > -__builtin_inff();
   const float sum = exponentials<V, L>(x, counted ? top : 0.f);
   const float inv = counted ? 1.f / sum : 0.f;
   float shift = 0.f;  // of all places, times p
-  float pull[V];
   if (a.dlosses) {
-    const float tokens = (float)a.counts[E], per = tokens > 0.f ? 1.f / tokens : 0.f;
-    const float scale = a.dlosses[0] * a.coef * per * per;
+    const float per = tokens > 0.f ? 1.f / tokens : 0.f, scale = balance * a.coef * per * per;
     float dot = 0.f;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      const int e = (i / 4 * L + lane) * 4 + i % 4;
-      pull[i] = scale * (float)a.counts[e < E ? e : E - 1];
+      pull[i] *= scale;
       dot = __builtin_fmaf(x[i] * inv, pull[i], dot);
     }
-    shift = 2.f * a.dlosses[1] * per * (top + logf(sum)) - sum_lanes(dot, L);
+    shift = 2.f * squares * per * (top + logf(sum)) - sum_lanes(dot, L);
   } else {
 #pragma unroll
     for (int i = 0; i < V; ++i) pull[i] = 0.f;
   }
-  if (a.dweights) {
-    auto number = [&](int j) {
-      const int id = counted ? a.ids[n * k + j] : -1;
-      return (uint32_t)id < (uint32_t)E ? id : -1;
-    };
+  if (weighed) {
     float from = top, over = sum;
     if (a.normalise) {
-      from = -__builtin_inff();
-      for (int j = lane; j < k; j += L) {
+      from = l0;
+      for (int j = lane + L; j < k; j += L) {
         const int id = number(j);
-        if (id >= 0) from = fmaxf(from, logit_at(a, row, id));
+        if (id >= 0) from = fmaxf(from, place[place_of(id)]);
       }
       from = max_lanes(from, L);
-      over = 0.f;
-      for (int j = lane; j < k; j += L) {
+    }
+    const float e0 = id0 >= 0 ? __expf(l0 - from) : 0.f;
+    if (a.normalise) {
+      over = e0;
+      for (int j = lane + L; j < k; j += L) {
         const int id = number(j);
-        if (id >= 0) over += __expf(logit_at(a, row, id) - from);
+        if (id >= 0) over += __expf(place[place_of(id)] - from);
       }
       over = sum_lanes(over, L);
     }
-    float dot = 0.f;
-    for (int j = lane; j < k; j += L) {
+    const float w0 = id0 >= 0 ? e0 / over : 0.f;
+    float dot = w0 * d0;
+    for (int j = lane + L; j < k; j += L) {
       const int id = number(j);
-      if (id >= 0) dot = __builtin_fmaf(__expf(logit_at(a, row, id) - from) / over, a.dweights[n * k + j], dot);
+      if (id >= 0) dot = __builtin_fmaf(__expf(place[place_of(id)] - from) / over, a.dweights[n * k + j], dot);
     }
     dot = sum_lanes(dot, L);
+    const float less = a.normalise ? dot : 0.f;
+    if (!a.normalise) shift -= dot;
+    // The row makes room.  Choices behind a lane's first are added from the logits in memory.
     __builtin_amdgcn_wave_barrier();
-    for (int j = lane; j < k; j += L) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) place[i * L + lane] = 0.f;
+    __builtin_amdgcn_wave_barrier();
+    if (id0 >= 0) atomicAdd(&place[place_of(id0)], w0 * (d0 - less));
+    for (int j = lane + L; j < k; j += L) {
       const int id = number(j);
-      if (id < 0) continue;
-      const float w = __expf(logit_at(a, row, id) - from) / over;
-      const int quad = id >> 2;
-      const int at = (quad / L * 4 + (id & 3)) * L + quad % L;
-      atomicAdd(&direct[at], w * (a.dweights[n * k + j] - (a.normalise ? dot : 0.f)));
+      if (id >= 0) atomicAdd(&place[place_of(id)], __expf(logit_at(a, row, id) - from) / over * (a.dweights[n * k + j] - less));
     }
     __builtin_amdgcn_wave_barrier();
-    if (!a.normalise) shift -= dot;
   }
   if (!here) return;
   char* out = a.dlogits + n * a.ld_out;
@@ -544,7 +572,8 @@ __global__ __launch_bounds__(256) void choose_backward_kernel(const ChooseArgs a
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
       const int i = 4 * u + c;
-      d[c] = counted ? __builtin_fmaf(x[i] * inv, pull[i] + shift, direct[i * L + lane]) : 0.f;
+      const float chosen = weighed ? place[i * L + lane] : 0.f;
+      d[c] = counted ? __builtin_fmaf(x[i] * inv, pull[i] + shift, chosen) : 0.f;
     }
     if (a.dtype == EBAG_F32) {
       if (e + 4 <= E) {
