@@ -401,59 +401,72 @@ __global__ __launch_bounds__(TOTALS ? 1024 : 256) void choose_kernel(const Choos
   }
 }
 
-// The workgroups' totals, summed in their order: a workgroup has 32 columns of them, eight
-// threads each.  The last one to be done, whichever it is, adds up what they made of the
-// balance loss, in their order.
-__global__ __launch_bounds__(256) void choose_join_kernel(const ChooseArgs a, int parts) {
-  __shared__ float sums[8][kJoinColumns];
-  __shared__ int32_t counts[8][kJoinColumns];
-  const int E = a.E, column = threadIdx.x % kJoinColumns, slice = threadIdx.x / kJoinColumns;
-  const int e = blockIdx.x * kJoinColumns + column;
+// The workgroups' totals, summed in their order: a workgroup has `columns` of them, eight threads or more each.  One
+// workgroup that has all columns makes the losses of them; of several the last one to be done, whichever it is, adds up
+// what all made of the balance loss, in their order.  (16384 tokens, 256 experts, 256 parts: nine workgroups of 32 columns
+// and 256 threads 4.8 us, of 1024 threads 5.8, one workgroup alone 12; 60 experts, 141 parts: one of 1024 threads 3.3, two
+// of 256 4.4.)
+__global__ __launch_bounds__(1024) void choose_join_kernel(const ChooseArgs a, int parts, int columns) {
+  __shared__ float sums[1024];
+  __shared__ int32_t counts[1024];
+  __shared__ float waves[16];
+  const int E = a.E, column = threadIdx.x & (columns - 1), slices = blockDim.x / columns, slice = threadIdx.x / columns;
+  const int e = blockIdx.x * columns + column;
   const float* work = parts_of(a.work);
   float s = 0.f;
   int32_t c = 0;
   if (e <= E) {
     const int32_t* numbers = reinterpret_cast<const int32_t*>(work) + (size_t)parts * (E + 1);
 #pragma unroll 16
-    for (int w = slice; w < parts; w += 8) {
+    for (int w = slice; w < parts; w += slices) {
       s += work[(size_t)w * (E + 1) + e];
       c += numbers[(size_t)w * (E + 1) + e];
     }
   }
-  sums[slice][column] = s;
-  counts[slice][column] = c;
+  sums[threadIdx.x] = s;
+  counts[threadIdx.x] = c;
   __syncthreads();
-  if (threadIdx.x >= 64) return;
+  const bool alone = gridDim.x == 1;
   float part = 0.f;
   if (slice == 0 && e <= E) {
-    for (int i = 1; i < 8; ++i) {
-      s += sums[i][column];
-      c += counts[i][column];
+    for (int i = 1; i < slices; ++i) {
+      s += sums[i * columns + column];
+      c += counts[i * columns + column];
     }
     // At device scope: another workgroup reads the last column's.
     __hip_atomic_store(&a.sums[e], s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __hip_atomic_store(&a.counts[e], c, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     if (e < E) part = (float)c * s;
+    if (alone && e == E) {
+      sums[0] = s;  // column 0's own is in its thread's register
+      counts[0] = c;
+    }
   }
   part = sum_lanes(part, 64);
-  uint32_t done = 0;
-  if (threadIdx.x == 0) {
-    __hip_atomic_store(&a.work[1 + blockIdx.x], part, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  }
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");
-  if (threadIdx.x == 0)
-    done = __hip_atomic_fetch_add(reinterpret_cast<uint32_t*>(a.work), 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
-  if (__builtin_amdgcn_readfirstlane(done) + 1 != gridDim.x) return;
-  if (threadIdx.x == 0) {
-    float all = 0.f;
+  if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = part;
+  __syncthreads();
+  if (threadIdx.x) return;
+  float all = 0.f;
+  for (int w = 0; w < (int)blockDim.x / 64; ++w) all += waves[w];
+  float squares;
+  int32_t T;
+  if (alone) {
+    squares = sums[0];
+    T = counts[0];
+  } else {
+    __hip_atomic_store(&a.work[1 + blockIdx.x], all, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    // All 32 columns are this thread's wave's: its release waits for their stores.
+    const uint32_t done = __hip_atomic_fetch_add(reinterpret_cast<uint32_t*>(a.work), 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+    if (done + 1 != gridDim.x) return;
+    all = 0.f;
     for (unsigned i = 0; i < gridDim.x; ++i)
       all += __hip_atomic_load(&a.work[1 + i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    const int32_t T = __hip_atomic_load(&a.counts[E], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    const float squares = __hip_atomic_load(&a.sums[E], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    const float per = T ? 1.f / (float)T : 0.f;
-    a.losses[0] = a.coef * all * per * per;
-    a.losses[1] = squares * per;
+    T = __hip_atomic_load(&a.counts[E], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    squares = __hip_atomic_load(&a.sums[E], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
+  const float per = T ? 1.f / (float)T : 0.f;
+  a.losses[0] = a.coef * all * per * per;
+  a.losses[1] = squares * per;
 }
 
 // With a_e = dlosses[0] E / (k T^2) counts[e], q = 2 dlosses[1] lse / T and p the
@@ -725,7 +738,8 @@ int ebag_a2a_moe_choose(ebag_a2a_moe_t h, const void* logits, int64_t ldl, int32
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return hipf(e, "launch the choice");
   if (!totals || wgs == 1) return EBAG_OK;
-  hipLaunchKernelGGL(choose_join_kernel, dim3(a.E / kJoinColumns + 1), dim3(256), 0, stream, a, (int)wgs);
+  const int columns = a.E < 64 ? 64 : a.E < 128 ? 128 : kJoinColumns;
+  hipLaunchKernelGGL(choose_join_kernel, dim3(a.E / columns + 1), dim3(columns == kJoinColumns ? 256 : 1024), 0, stream, a, (int)wgs, columns);
   e = hipGetLastError();
   return e == hipSuccess ? EBAG_OK : hipf(e, "launch the choice's totals");
 }

@@ -98,14 +98,14 @@ __device__ __forceinline__ void q8_load8(const char* row, int at, int K, float* 
   }
 }
 
-// The whole number nearest to x / scale, halves to even: what the product with the reciprocal gives is at most one
-// off, and x less that many scales, exact up to its sign and its order with scale / 2, says which way.
 __device__ __forceinline__ float q8_scale(uint32_t top) {  // of a row whose largest size has these bits
   return top >= 0x7f800000u ? __builtin_nanf("") : __uint_as_float(top) / 127.f;
 }
 
+// The whole number nearest to x / scale, halves to even: what the product with the reciprocal gives is at most one
+// off, and x less that many scales, exact up to its sign and its order with scale / 2, says which way.
 struct Q8Rounder {
-  float scale, inv, half, factor;
+  float scale, inv, half, near, factor;
   bool any;
   __device__ __forceinline__ Q8Rounder(float s) {
     // Scales so small that their reciprocal would not be a number, or their half not exact, are taken 2^64 times.
@@ -114,6 +114,7 @@ struct Q8Rounder {
     any = s > 0.f;  // not NaN
     inv = any ? 1.f / scale : 0.f;
     half = 0.5f * scale;
+    near = any && factor == 1.f ? half * (1.f - 0x1p-12f) : 0.f;
   }
   __device__ __forceinline__ int code(float x) const {
     x *= factor;
@@ -124,10 +125,30 @@ struct Q8Rounder {
   }
 };
 
+// Eight elements to codes.  Where none of them is next to the middle of two codes, the nearest number to the product with
+// the reciprocal is right as it is; it stands in the low bits of its sum with 1.5 * 2^23 (5 instructions an element
+// instead of 20; 8192 rows of 8192 bf16 50 -> 46 us).
 __device__ __forceinline__ void q8_store8(int8_t* to, const Q8Rounder& r, const float* f) {
-  uint32_t w[2] = {0, 0};
+  constexpr float kShift = 12582912.f;
+  uint32_t bits[8], w[2] = {0, 0};
+  float worst = 0.f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) w[i / 4] |= ((uint32_t)r.code(f[i]) & 0xffu) << (8 * (i % 4));
+  for (int i = 0; i < 8; ++i) {
+    const float t = fmaf(f[i], r.inv, kShift);
+    worst = fmaxf(worst, fabsf(fmaf(-(t - kShift), r.scale, f[i])));
+    bits[i] = __float_as_uint(t);
+  }
+  if (worst < r.near) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t lo = __builtin_amdgcn_perm(bits[4 * i + 1], bits[4 * i], 0x0c0c0400u);
+      const uint32_t hi = __builtin_amdgcn_perm(bits[4 * i + 3], bits[4 * i + 2], 0x04000c0cu);
+      w[i] = lo | hi;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i / 4] |= ((uint32_t)r.code(f[i]) & 0xffu) << (8 * (i % 4));
+  }
   *reinterpret_cast<uint2*>(to) = uint2{w[0], w[1]};
 }
 

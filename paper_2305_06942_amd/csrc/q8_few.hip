@@ -34,7 +34,7 @@ struct Few {
   static constexpr int X_COPIES = X_ROWS / 8 / WW, COPIES = 2 * RT + X_COPIES;           // of a wave, eight rows each
   static_assert(X_COPIES * 8 * WW == X_ROWS, "");
   // Three workgroups on a CU, or two, or one.
-  static constexpr int RING = kCuLds / (STAGE * 9 <= kCuLds ? 3 : STAGE * 6 <= kCuLds ? 2 : 1) - (OWN ? 4096 : 0);
+  static constexpr int RING = OWN ? 64 * 1024 : kCuLds / (STAGE * 9 <= kCuLds ? 3 : STAGE * 6 <= kCuLds ? 2 : 1);
   static constexpr int FIT = RING / STAGE, MOST = 62 / COPIES + 2;
   static constexpr int STAGES = FIT < MOST ? FIT : MOST;
   static_assert(STAGES >= 3, "");
@@ -252,14 +252,17 @@ void launch(const Q8Args& a, unsigned grid, hipStream_t stream) {
   hipLaunchKernelGGL((q8_few_kernel<RT, NT, WW, WAVES, false>), dim3(grid), dim3(64 * WAVES), (Few<RT, NT, WW, WAVES, false>::LDS), stream, a);
 }
 
+constexpr int kOwnWaves = 8;
 int own_bytes(const Q8Args& a) {  // of LDS, behind the ring
   const int raw = a.K * (a.x_type == EBAG_F32 ? 4 : 2);
-  return (int)a.rows * ((int)a.pitch + (raw + 1023) / 1024 * 1024) + 4 * kQ8Own * (1 + 4);
+  return (int)a.rows * ((int)a.pitch + (raw + 1023) / 1024 * 1024) + 4 * kQ8Own * (1 + kOwnWaves);
 }
 
 template <int RT, int WW>
 void launch_own(const Q8Args& a, unsigned grid, hipStream_t stream) {
-  hipLaunchKernelGGL((q8_few_kernel<RT, 1, WW, 4, true>), dim3(grid), dim3(256), (Few<RT, 1, WW, 4, true>::LDS) + own_bytes(a), stream, a);
+  constexpr int WAVES = kOwnWaves / RT;
+  hipLaunchKernelGGL((q8_few_kernel<RT, 1, WW, WAVES, true>), dim3(grid), dim3(64 * WAVES), (Few<RT, 1, WW, WAVES, true>::LDS) + own_bytes(a),
+                     stream, a);
 }
 
 template <int RT>
@@ -281,11 +284,11 @@ void launch(const Q8Args& a, int x_tiles, int waves, unsigned grid, hipStream_t 
 
 }  // namespace
 
-// Up to two thirds of a CU's LDS next to the ring, and x as copies take it.
+// What the ring leaves of a CU's LDS, and x as copies take it.
 bool q8_own_fits(const Q8Args& a) {
   const int elt = a.x_type == EBAG_F32 ? 4 : 2;
   return a.x && a.rows <= kQ8Own && !a.offsets && (int64_t)a.K * elt % 16 == 0 && a.ldx % 16 == 0 &&
-         reinterpret_cast<uintptr_t>(a.x) % 16 == 0 && own_bytes(a) <= kCuLds * 2 / 3;
+         reinterpret_cast<uintptr_t>(a.x) % 16 == 0 && own_bytes(a) <= kCuLds - 64 * 1024;
 }
 
 void launch_q8_own(const Q8Args& a, int tiles, int waves, unsigned grid, hipStream_t stream) {
