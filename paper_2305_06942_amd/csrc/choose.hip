@@ -3,8 +3,6 @@
 // totals with the two losses made of them, and the gradients of all of it.
 #include <hip/hip_runtime.h>
 
-#include <climits>
-
 #include "common.h"
 #include "ebag_a2a.h"
 #include "lanes.h"
@@ -18,6 +16,7 @@ namespace {
 // L lanes (4 to 64) have a token, V of its logits each, four neighbouring ones at
 // a time: logit (u * L + lane) * 4 + c in place 4 u + c.
 constexpr int kMostParts = 256;   // workgroups whose totals are joined
+constexpr int kMostGroups = 1 << 22;  // of a launch, whose threads are numbered in 32 bits
 constexpr int kJoinColumns = 32;  // of a workgroup that joins them
 constexpr int kMostJoins = (kMaxExperts + kJoinColumns) / kJoinColumns;
 
@@ -725,11 +724,11 @@ int ebag_a2a_moe_choose(ebag_a2a_moe_t h, const void* logits, int64_t ldl, int32
   const int groups = threads / lanes;
   int64_t wgs = (tokens + groups - 1) / groups;
   if (wgs < 1) wgs = 1;
-  if (totals && wgs > kMostParts) {
-    a.turns = (int32_t)((wgs + kMostParts - 1) / kMostParts);
+  const int64_t most = totals ? kMostParts : kMostGroups;
+  if (wgs > most) {
+    a.turns = (int32_t)((wgs + most - 1) / most);
     wgs = (wgs + a.turns - 1) / a.turns;
   }
-  if (wgs > INT_MAX) return fail(EBAG_EINVAL, "too many tokens for one launch");
   size_t lds = (size_t)groups * a.k * 8;
   if (totals) lds += (size_t)(a.E + 1) * 4 * (1 + threads / 64) + 64;
   const bool merge = a.k > 2 && a.k <= 8;
@@ -765,12 +764,20 @@ int ebag_a2a_moe_choose_backward(ebag_a2a_moe_t h, const void* logits, int64_t l
   a.dlosses = dlosses;
   a.dlogits = static_cast<char*>(dlogits);
   a.ld_out = lddl * elt;
-  const int groups = 256 / lanes;
-  const int64_t wgs = (tokens + groups - 1) / groups;
-  if (wgs > INT_MAX) return fail(EBAG_EINVAL, "too many tokens for one launch");
-  hipLaunchKernelGGL(pick_backward(values, lanes), dim3((unsigned)wgs), dim3(256), 0, stream, a);
-  const hipError_t e = hipGetLastError();
-  return e == hipSuccess ? EBAG_OK : hipf(e, "launch the choice's gradient");
+  const int64_t groups = 256 / lanes, step = kMostGroups * groups;
+  for (;;) {
+    const int64_t wgs = (a.tokens + groups - 1) / groups;
+    hipLaunchKernelGGL(pick_backward(values, lanes), dim3((unsigned)(wgs < kMostGroups ? wgs : kMostGroups)), dim3(256), 0, stream, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return hipf(e, "launch the choice's gradient");
+    if (a.tokens <= step) return EBAG_OK;
+    a.tokens -= step;
+    a.logits += step * a.ld;
+    a.dlogits += step * a.ld_out;
+    if (a.live) a.live += step;
+    if (a.ids) a.ids += step * a.k;
+    if (a.dweights) a.dweights += step * a.k;
+  }
 }
 
 }  // extern "C"

@@ -128,8 +128,7 @@ int launch_round(const gemv_ar_q8_plan* h, const void* x, int64_t ldx, int64_t r
   a.K = (int32_t)h->K;
   a.units = (int32_t)(h->pitch / 8);
   const bool wave = h->K <= 64 * 8 * kHeld && (rows >= 2048 || h->K <= 256);
-  const int64_t per_wg = wave ? kRoundThreads / 64 : 1, wgs = (rows + per_wg - 1) / per_wg;
-  if (wgs > INT_MAX) return fail(EBAG_EUNSUPPORTED, "too many rows for one launch");
+  const int64_t per_wg = wave ? kRoundThreads / 64 : 1;
   void (*fn)(const RoundArgs) = h->dtype == EBAG_F32   ? wave ? q8_round_kernel<0, true> : q8_round_kernel<0, false>
                                 : h->dtype == EBAG_F16 ? wave ? q8_round_kernel<1, true> : q8_round_kernel<1, false>
                                 : wave                 ? q8_round_kernel<2, true>
@@ -137,9 +136,18 @@ int launch_round(const gemv_ar_q8_plan* h, const void* x, int64_t ldx, int64_t r
   // A few long rows: a thread for every 8 elements, up to 1024 (64 rows of 8192 bf16 with 256 threads each 6.7 us).
   int threads = kRoundThreads;
   while (!wave && rows < 1024 && threads < 1024 && threads < a.units) threads *= 2;
-  hipLaunchKernelGGL(fn, dim3((unsigned)wgs), dim3(threads), 0, stream, a);
-  const hipError_t e = hipGetLastError();
-  return e == hipSuccess ? EBAG_OK : hipf(e, "launch the rounding to 8 bits");
+  constexpr int64_t kMost = 1 << 22;  // workgroups of a launch, whose threads are numbered in 32 bits
+  for (int64_t left = rows; left > 0; left -= kMost * per_wg) {
+    const int64_t wgs = (left + per_wg - 1) / per_wg;
+    hipLaunchKernelGGL(fn, dim3((unsigned)(wgs < kMost ? wgs : kMost)), dim3(threads), 0, stream, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return hipf(e, "launch the rounding to 8 bits");
+    a.x += kMost * per_wg * a.ld;
+    a.codes += kMost * per_wg * a.pitch;
+    a.scales += kMost * per_wg;
+    a.rows -= kMost * per_wg;
+  }
+  return EBAG_OK;
 }
 
 int fill_args(const gemv_ar_q8_plan* h, const int8_t* codes, const float* scales, const void* x, int64_t ldx, int64_t x_rows,
@@ -192,7 +200,7 @@ int launch_few(Q8Args a, int x_tiles, hipStream_t stream) {
   const int64_t grid_tiles = (wave_tiles + waves - 1) / waves, eighths = (grid_tiles + 7) / 8;
   const int64_t group = a.offsets ? (a.rows > (int64_t)cols * a.experts ? 4 : 1) : slots < 8 ? slots : 8, groups = (slots + group - 1) / group;
   const int64_t grid = 8 * eighths * group * groups;
-  if (grid > INT_MAX) return fail(EBAG_EUNSUPPORTED, "too many tiles for one launch");
+  if (grid > UINT32_MAX / 512) return fail(EBAG_EUNSUPPORTED, "too many tiles for one launch");
   a.by_tiles = make_divisor(eighths);
   a.tiles = (uint32_t)grid_tiles;
   a.by_group = make_divisor(group);
@@ -209,7 +217,7 @@ int launch_tile(Q8Args a, Q8Tile kind, hipStream_t stream) {
   const int64_t per_wg = q8_tile_w(kind) / (a.glu ? 2 : 1), tiles = (a.out_rows + per_wg - 1) / per_wg;
   const int64_t slots = a.offsets ? most_tiles(a.rows, a.experts, x_rows) : (a.rows + x_rows - 1) / x_rows;
   const int64_t grid = (slots + 3) / 4 * 4 * tiles;
-  if (grid > INT_MAX) return fail(EBAG_EUNSUPPORTED, "too many tiles for one launch");
+  if (grid > UINT32_MAX / 512) return fail(EBAG_EUNSUPPORTED, "too many tiles for one launch");
   a.by_tiles = make_divisor(tiles);
   a.whole = (uint32_t)(grid / 256 * 256);
   launch_q8_tile(a, kind, (unsigned)grid, stream);
