@@ -240,7 +240,7 @@ __global__ __launch_bounds__(64 * WAVES) void q8_few_kernel(const Q8Args a) {
         float v = (float)sum[b][t][i] * (xs * ws);
         if (RT > 1 && pair == 2) {
           const float up = (float)sum[b + 1 < RT ? b + 1 : b][t][i] * (xs * wu);
-          v = (a.y_type == EBAG_F32 ? silu<true>(v) : silu<false>(v)) * up;
+          v = (a.y_type == EBAG_F32 ? q8_silu<true>(v) : q8_silu<false>(v)) * up;
         }
         q8_store(a, n, m, v);
       }

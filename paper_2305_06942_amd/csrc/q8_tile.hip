@@ -159,6 +159,12 @@ __global__ __launch_bounds__(kThreads, 1) void q8_tile_kernel(const Q8Args a) {
       __builtin_amdgcn_sched_barrier(0);  // in the order in which they are waited for
     }
   }
+  float xs[TX];  // here already, as a row's number may have to be loaded first
+#pragma unroll
+  for (int t = 0; t < TX; ++t) {
+    const uint32_t n = first + wave_x * (16 * TX) + 16 * t + r16;
+    xs[t] = a.xs[q8_x_row(a, n < end ? n : end - 1)];
+  }
   __syncthreads();
 #pragma unroll
   for (int b = 0; b < TW; ++b) fetch_w(b, piece_of(0, 0));
@@ -180,7 +186,7 @@ __global__ __launch_bounds__(kThreads, 1) void q8_tile_kernel(const Q8Args a) {
   const int64_t left = a.out_rows - m0;                          // columns of y from the wave's first on
   const float* scales = a.scales + (int64_t)expert * a.M;
   auto col_of = [&](int b) { return (GLU ? b / 4 * 2 + b % 2 : b) * 16 + 4 * quarter; };
-  float ws[TW][4], xs[TX];
+  float ws[TW][4];
 #pragma unroll
   for (int b = 0; b < TW; ++b) {
     const int col = col_of(b);
@@ -191,11 +197,6 @@ __global__ __launch_bounds__(kThreads, 1) void q8_tile_kernel(const Q8Args a) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) ws[b][i] = from[col + i < left ? m0 + col + i : a.out_rows - 1];
     }
-  }
-#pragma unroll
-  for (int t = 0; t < TX; ++t) {
-    const uint32_t n = first + wave_x * (16 * TX) + 16 * t + r16;
-    xs[t] = a.xs[q8_x_row(a, n < end ? n : end - 1)];
   }
   work(step & 1, step, std::false_type(), std::false_type());
 #pragma unroll
@@ -216,7 +217,7 @@ __global__ __launch_bounds__(kThreads, 1) void q8_tile_kernel(const Q8Args a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           v[i] = (float)sum[b][t][i] * (xs[t] * ws[b][i]);
-          if (GLU) v[i] = silu<DT == 0>(v[i]) * ((float)sum[GLU ? b + 2 : b][t][i] * (xs[t] * ws[GLU ? b + 2 : b][i]));
+          if (GLU) v[i] = q8_silu<DT == 0>(v[i]) * ((float)sum[GLU ? b + 2 : b][t][i] * (xs[t] * ws[GLU ? b + 2 : b][i]));
         }
         char* to = mine + ((t - t0) * 16 + r16) * PITCH + col_of(b) * ELT;
         const vec16 p = Type<DT>::narrow(v);
