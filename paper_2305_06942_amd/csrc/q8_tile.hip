@@ -1,4 +1,12 @@
 // Products with 8-bit weights for many rows of x: the matrix-product kernel.
+//
+// y[n][m] = xs[n] scales[m] sum_k xq[n][k] codes[m][k], the sums exact in 32 bits.  Bound by the matrix
+// instructions, and those by power: with numbers that change, 16x16x64 ones alone run at 3700 to 3900 Tops
+// (4900 at 2.4 GHz with operands that never change; 32x32x32 ones 3430).  Of the about 2800 cycles
+// of a step of 128 columns (256 x 256 sums) 2092 are theirs; loads from LDS add 120, stores into it 360, loads from memory
+// 210, measured one by one.  Rows from memory straight into LDS were no faster (22 bytes a cycle of a CU, where the
+// way through registers has 70), nor operands two steps ahead in registers (spills).  8192 x 8192 x 8192 in bf16: 412 us, 2670
+// Tops, and about 420 in a run of many.  32768 x 4096 x 2048: 271 us, of which beginnings 30 and results 50.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
