@@ -230,7 +230,7 @@ void gemv_ar_q4_destroy(gemv_ar_q4_t h);
  * times the product of its scales, and once to y's type, the plan's or fp32.  Row r
  * of x starts at element r * ldx, of y at element r * ldy; neither needs an alignment
  * beyond its elements'; codes and xq are 16-byte aligned.  Outputs must not overlap inputs.
- * Results do not depend on the other rows' values and are the same bits on every run.
+ * A row's results are the same bits on every run and whatever rows are with it.
  */
 typedef struct gemv_ar_q8_plan* gemv_ar_q8_t;
 

@@ -43,7 +43,8 @@ struct Q8Args {
   int32_t K;
   Divisor by_choices;
   Divisor by_tiles;         // workgroups that share the rows of x, each with its rows of weights: of the kernel for few
-                            // rows an eighth of them
+                            // rows those of an XCD, or all
+  int32_t spread;           // of the kernel for few rows: 3, neighbouring tiles on the eight XCDs, or 0, no order
   uint32_t tiles;           // the kernel for few rows: all of them
   Divisor by_group;         // and slots that have their turn with a workgroup's weights one after the other
   // The matrix-product kernel.
@@ -56,12 +57,19 @@ __device__ __forceinline__ int64_t q8_x_row(const Q8Args& a, uint32_t n) {
   return row < a.x_rows ? row : a.x_rows - 1;
 }
 
+// A result in fp32.  Left to itself the compiler rounds some products to fp16 at once and some over fp32, and a row's results
+// would differ in their last bit from kernel to kernel.
+__device__ __forceinline__ float q8_result(float v) {
+  asm("" : "+v"(v));
+  return v;
+}
+
 __device__ __forceinline__ void q8_store(const Q8Args& a, uint32_t n, int64_t m, float v) {
   char* p = a.y + n * a.ldy;
   if (a.y_type == EBAG_F32)
     reinterpret_cast<float*>(p)[m] = v;
   else if (a.y_type == EBAG_F16)
-    reinterpret_cast<_Float16*>(p)[m] = Type<1>::narrow(v);
+    reinterpret_cast<_Float16*>(p)[m] = Type<1>::narrow(q8_result(v));
   else
     reinterpret_cast<__bf16*>(p)[m] = Type<2>::narrow(v);
 }

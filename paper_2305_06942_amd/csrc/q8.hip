@@ -196,10 +196,14 @@ int launch_few(Q8Args a, int x_tiles, hipStream_t stream) {
   const int64_t wave_tiles = (a.out_rows + 15) / 16, used = a.offsets ? (a.rows + cols - 1) / cols : slots;
   const int most = x_tiles == 1 ? 2 : x_tiles == 2 ? 4 : 8;
   int waves = x_tiles == 8 ? 4 : 1;
-  while (waves < most && wave_tiles * used >= 200 * 2 * waves) waves *= 2;
-  const int64_t grid_tiles = (wave_tiles + waves - 1) / waves, eighths = (grid_tiles + 7) / 8;
-  const int64_t group = a.offsets ? (a.rows > (int64_t)cols * a.experts ? 4 : 1) : slots < 8 ? slots : 8, groups = (slots + group - 1) / group;
-  const int64_t grid = 8 * eighths * group * groups;
+  const int64_t lines = a.pitch / kQ8Line;  // not more waves to the columns than lines (77 rows x 2610 x 94, 17 experts: 44 -> 10 us)
+  while (waves < most && (wave_tiles * used >= 200 * 2 * waves || lines * waves < 4)) waves *= 2;
+  // A few tiles are not an eighth for each XCD: they are left to all of them (2920 rows x 54 x 2587: 15.3 -> 7.7 us).
+  const int64_t grid_tiles = (wave_tiles + waves - 1) / waves;
+  a.spread = grid_tiles < 64 ? 0 : 3;
+  const int64_t eighths = ((grid_tiles - 1) >> a.spread) + 1;
+  const int64_t group = !a.spread ? 1 : a.offsets ? (a.rows > (int64_t)cols * a.experts ? 4 : 1) : slots < 8 ? slots : 8, groups = (slots + group - 1) / group;
+  const int64_t grid = (eighths << a.spread) * group * groups;
   if (grid > UINT32_MAX / 512) return fail(EBAG_EUNSUPPORTED, "too many tiles for one launch");
   a.by_tiles = make_divisor(eighths);
   a.tiles = (uint32_t)grid_tiles;
@@ -228,24 +232,28 @@ int launch_tile(Q8Args a, Q8Tile kind, hipStream_t stream) {
 // Which kernel, by a model of measured times in us.  A kernel has `cols` rows of x and `rows` of weights to a workgroup.
 // `fix` is its beginning and end; K = 4096 (times K / 4096 for others) takes at least `least`, a workgroup's own time, and
 // otherwise `start` and `each` ns for every 16 x 16 sums, or `round` for every 256 workgroups of the largest tiles, one
-// to a CU.  Where the weights are more than the caches hold, memory's rate bounds all of them, `rate` in TB/s, at 1.5 times
+// to a CU.  With a shorter K the results' own time shows, `ends` ns for 16 x 16 of them, and the largest tiles take at
+// least `floor`.  Where the weights are more than the caches hold, memory's rate bounds all of them, `rate` in TB/s, at 1.5 times
 // the bytes with two tiles of x and so on in the kernel that streams (its tiles of x share weights in the L2 by half).
-//   bf16 x 4096 x 4096, in us by 16, 32, 64 and 128 rows of x in the streaming kernel, 256 x 64, 512 x 128 and 256 x 256:
-//     64 rows 9.8, 10.0, 11.5, 24, 20.6, 48, 46; 256 rows 25.5, 16.6, 18.8, 27, 21.1, 50, 48; 512 rows 47, 30, 20.2, 29, 21.8,
-//     50, 49; 2048 rows 164, 86, 53, 60, 41, 55, 51; 4096 rows 308, 155, 101, 114, 78, 64, 60
-//   128 rows x 65536 x 8192: 355, 207, 143, 120, 194, 213, 348
-//   gated experts of 2 x 1024 x 2048: 128 of them with 2 rows each 87, 90, 227, 139, 87, 99, 143; 64 with 32 rows each 91, 64,
-//     60, 92, 53, 59, 77; with 256 rows each 462, 243, 189, 174, 125, 131, 160
+// Fitted to 129 products in bf16 with every kernel, K from 80 to 10128: what it takes is 1 % slower than the fastest of the
+// seven on average, 33 % at most.  Some of them, in us by 16, 32, 64 and 128 rows of x in the streaming kernel, 256 x 64,
+// 512 x 128 and 256 x 256:
+//   4096 x 4096: 64 rows 9.5, 9.9, 11.5, 24, 20.3, 48, 45; 256 rows 25, 16.7, 18.3, 27, 21, 50, 48; 512 rows 45, 30.5, 20, 28.5, 22.7,
+//     50, 48; 2048 rows 167, 88, 56, 63, 41, 56, 52
+//   128 rows x 65536 x 8192: 354, 206, 143, 120, 194, 215, 347; 512 rows x 20000 x 256: 56, 27, 21, 30, 14, 18, 27
+//   2920 rows x 54 x 2587: 7.7, 10.4, 11.8, 20, 17, 44, 42
+//   gated experts of 2 x 1024 x 2048: 128 of them with 2 rows each 85, 88, 214, 140, 85, 98, 133; 64 with 32 rows each 88, 62,
+//     65, 88, 53, 58, 74; of 2 x 2048 x 2048, 64 with 512 rows each 1724, 850, 648, 568, 387, 377, 384
 struct Kernel {
   int x_tiles;  // of 16 rows, in the streaming kernel; 0: the matrix-product kernel
   Q8Tile tile;
-  double cols, rows, fix, least, start, each, round, rate;
+  double cols, rows, fix, floor, least, start, each, ends, round, rate;
 };
 constexpr Kernel kKernels[] = {
-    {1, Q8_256x64, 16, 16, 3, 1.5, 1.5, 5.2, 0, 5.6},   {2, Q8_256x64, 32, 16, 3, 4, 4, 2.75, 0, 5.6},
-    {4, Q8_256x64, 64, 16, 3, 7, 7, 1.3, 0, 5.6},       {8, Q8_256x64, 128, 16, 3, 21, 21, 1.0, 0, 4.5},
-    {0, Q8_256x64, 64, 256, 4, 16.5, 1, 1.17, 0, 5.4},  {0, Q8_512x128, 128, 512, 8, 40, 0, 0, 53, 2.5},
-    {0, Q8_256x256, 256, 256, 9, 37, 0, 0, 48, 1.5}};
+    {1, Q8_256x64, 16, 16, 3.1, 0, 3.6, 1, 4.4, 1.7, 0, 5.6},      {2, Q8_256x64, 32, 16, 3.9, 0, 3.3, 4.1, 2.1, 0.5, 0, 5.6},
+    {4, Q8_256x64, 64, 16, 5.2, 0, 4.8, 4.3, 1.9, 0.3, 0, 5.6},    {8, Q8_256x64, 128, 16, 4.9, 0, 22, 0, 1.6, 0.45, 0, 4.5},
+    {0, Q8_256x64, 64, 256, 5.3, 0, 18, 2.5, 0.9, 0.18, 0, 5.4},   {0, Q8_512x128, 128, 512, 4.2, 17, 42, 0, 0, 0.3, 58, 2.5},
+    {0, Q8_256x256, 256, 256, 7.5, 14, 43, 0, 0, 0.25, 50, 1.5}};
 
 double time_of(const Kernel& k, const Q8Args& a) {
   const double M = (double)a.M, scale = (double)a.pitch / 4096;
@@ -257,6 +265,8 @@ double time_of(const Kernel& k, const Q8Args& a) {
   const double wgs = std::ceil(M / k.rows) * slots, sums = std::ceil(M / k.rows) * (k.rows / 16) * slots * (k.cols / 16);
   double t = k.round ? std::ceil(wgs / 256) * k.round : k.start + sums * k.each * 1e-3;
   t = k.fix + scale * (t < k.least ? k.least : t);
+  if (scale < 1) t += sums * k.ends * 1e-3 * (1 - scale);
+  if (t < k.floor) t = k.floor;
   const double bytes = used * M * (double)a.pitch;
   if (bytes > 128e6) {
     double memory = bytes / (k.rate * 1e6);

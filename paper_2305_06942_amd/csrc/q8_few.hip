@@ -87,10 +87,11 @@ __global__ __launch_bounds__(64 * WAVES) void q8_few_kernel(const Q8Args a) {
   const int lane = threadIdx.x & 63, r16 = lane & 15, quarter = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave_w = wave % WW, part = wave / WW;
   // Neighbouring workgroups are on different XCDs: an XCD has every eighth tile of weights, for a group of slots one after
-  // the other, so that the second slot of one matrix finds them in the XCD's L2.
-  const uint32_t block = blockIdx.x >> 3, chunk = divide_by(a.by_group, block), in_group = block - chunk * a.by_group.d;
+  // the other, so that the second slot of one matrix finds them in the XCD's L2.  Without spread all tiles of a slot follow
+  // one another.
+  const uint32_t block = blockIdx.x >> a.spread, chunk = divide_by(a.by_group, block), in_group = block - chunk * a.by_group.d;
   const uint32_t group = divide_by(a.by_tiles, chunk), eighth = chunk - group * a.by_tiles.d;
-  const uint32_t slot = group * a.by_group.d + in_group, tile = eighth * 8 + (blockIdx.x & 7);
+  const uint32_t slot = group * a.by_group.d + in_group, tile = (eighth << a.spread) + (blockIdx.x & ((1u << a.spread) - 1));
   if (tile >= a.tiles) return;
   int expert;
   uint32_t first, end;

@@ -226,6 +226,7 @@ __global__ __launch_bounds__(kThreads, 1) void q8_tile_kernel(const Q8Args a) {
         for (int i = 0; i < 4; ++i) {
           v[i] = (float)sum[b][t][i] * (xs[t] * ws[b][i]);
           if (GLU) v[i] = q8_silu<DT == 0>(v[i]) * ((float)sum[GLU ? b + 2 : b][t][i] * (xs[t] * ws[GLU ? b + 2 : b][i]));
+          if (DT == 1) v[i] = q8_result(v[i]);
         }
         char* to = mine + ((t - t0) * 16 + r16) * PITCH + col_of(b) * ELT;
         const vec16 p = Type<DT>::narrow(v);

@@ -168,3 +168,66 @@ def test_a_serving_layer_captured_and_replayed(bits, tokens):
         torch.cuda.synchronize()
         got = out.clone()
         assert torch.equal(got, layer(x, logits)), f"replay {turn}"
+
+
+VARIANTS = [  # rows, E, M, K, glu, type: a kernel each, between them every one that the choice of kernel has
+    (1492, 85, 118, 443, 0, "bfloat16"), (8660, 1, 18, 396, 1, "float16"), (14174, 6, 2, 140, 0, "float32"), (12217, 1, 2, 1, 1, "bfloat16"),
+    (1282, 36, 240, 15402, 0, "float16"), (45, 1, 10756, 12023, 1, "bfloat16"), (43685, 7, 2, 18608, 0, "bfloat16"),
+    (41197, 1, 2, 17042, 1, "float16"), (58524, 1, 2, 11262, 0, "float32"), (56416, 1, 22, 1, 1, "float32"), (58067, 1, 20, 1, 0, "bfloat16"),
+    (54563, 1, 34, 1, 1, "float16"), (33948, 1, 96, 789, 0, "float16"), (44343, 1, 66, 714, 1, "bfloat16"), (51518, 1, 52, 834, 0, "bfloat16"),
+    (56569, 3, 120, 1236, 1, "float16"), (20640, 1, 570, 2102, 0, "float16"), (59061, 1, 154, 2604, 1, "bfloat16"),
+    (1345, 1, 11456, 2955, 0, "bfloat16"), (1374, 1, 11372, 3459, 1, "float16"), (2300, 3, 9000, 2048, 0, "float32"),
+    (64, 1, 60000, 128, 0, "float16"), (35, 15, 3894, 336, 1, "bfloat16"), (77, 17, 2610, 94, 1, "float16")]
+
+
+@pytest.mark.parametrize("rows,E,M,K,glu,dtype", VARIANTS)
+def test_every_kernel_against_64_bits(rows, E, M, K, glu, dtype):
+    """The definition on the GPU in 64 bits: the sums are whole numbers below 2^53."""
+    import torch
+    from tests.test_gpu_q8 import U
+    rng = np.random.default_rng([98, rows, M, K])
+    gen = torch.Generator(device="cuda").manual_seed(rows + M)
+    plan = _plan(M, K, dtype, experts=E, glu=glu)
+    codes = torch.randint(-128, 128, (E, M, plan.pitch), dtype=torch.int8, device="cuda", generator=gen)
+    scales = (torch.rand((E, M), device="cuda", generator=gen) + 0.5) / (73 * K ** 0.5)
+    x = torch.randn((rows, K), device="cuda", generator=gen).to(getattr(torch, dtype))
+    xq, xs = _scratch(plan, rows)
+    plan.round(x, xq, xs)
+    y = torch.full((rows, plan.wide), float("nan"), dtype=x.dtype, device="cuda")
+    ends = np.array([0, rows]) if E == 1 else np.concatenate(([0], np.sort(rng.integers(0, rows, size=E - 1)), [rows - 3]))
+    if E == 1:
+        plan.forward(codes, scales, None, y, xq, xs)
+    else:
+        plan.experts(codes, scales, None, torch.from_numpy(np.minimum(ends, rows - 3).astype(np.int32)).cuda(), y, xq, xs)
+        assert y[rows - 3:].eq(0).all()
+    for e in range(E):
+        for at in range(int(ends[e]), min(int(ends[e + 1]), rows - 3 if E > 1 else rows), 8192):
+            n = slice(at, min(at + 8192, int(ends[e + 1]), rows - 3 if E > 1 else rows))
+            want = (xq[n, :K].double() @ codes[e, :, :K].double().t().contiguous()) * xs[n].double()[:, None] * scales[e].double()
+            b = 4 * U * want.abs() + 2.0 ** -149
+            if glu:
+                g, u, bg, bu = want[:, :M // 2], want[:, M // 2:], b[:, :M // 2], b[:, M // 2:]
+                act = g / (1 + torch.exp(-g))
+                ba = 1.1 * bg + (g.abs() + 8) * 2.0 ** -22 * act.abs()
+                want, b = act * u, ba * u.abs() + act.abs() * bu + ba * bu + U * (act * u).abs()
+            lo, hi, got = (want - b).to(x.dtype), (want + b).to(x.dtype), y[n]
+            ok = (lo <= got) & (got <= hi)
+            assert bool(ok.all()), f"{int((~ok).sum())} of {ok.numel()} outside, first {(~ok).nonzero()[0].tolist()} of expert {e}"
+    plan.close()
+
+
+@pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("M,K,glu", [(300, 700, 0), (3000, 200, 1), (9000, 512, 0), (514, 2048, 1)])
+def test_a_row_has_the_same_bits_whatever_rows_are_with_it(M, K, glu, dtype):
+    """One row to some thousands go through different kernels; sums are exact and the rest is the same steps."""
+    import torch
+    plan = _plan(M, K, dtype, glu=glu)
+    w = Weights(np.random.default_rng(99), plan, M, K)
+    x = torch.randn((5000, K), device="cuda").to(getattr(torch, dtype))
+    first = None
+    for rows in (5000, 1, 2, 3, 16, 17, 40, 64, 100, 257, 700, 2049):
+        y = torch.full((rows, plan.wide), float("nan"), dtype=x.dtype, device="cuda")
+        plan.forward(w.codes, w.scales, x[:rows], y, *_scratch(plan, rows))
+        first = y if first is None else first
+        assert torch.equal(y, first[:rows]), f"{rows} rows"
+    plan.close()
