@@ -37,8 +37,7 @@ struct Q8Args {
   int32_t experts;
   int32_t glu;
   int32_t y_type;
-  const char* x;            // rows to be rounded by the product itself (kQ8Own at most, launch_q8_own alone)
-  int64_t ldx;              // bytes
+  const char* x;            // a row to be rounded by the product itself (launch_q8_own alone)
   int32_t x_type;
   int32_t K;
   Divisor by_choices;
@@ -175,8 +174,7 @@ constexpr int q8_tile_x(Q8Tile t) { return t == Q8_256x64 ? 64 : t == Q8_512x128
 
 // tiles: of 16 rows of weights of a wave; x_tiles: of 16 rows of x; waves: of four, that have different rows of weights.
 void launch_q8_few(const Q8Args& a, int tiles, int x_tiles, int waves, unsigned grid, hipStream_t stream);
-// The same for at most kQ8Own rows of x of any type, of whole 16-byte vectors on 16-byte boundaries.
-constexpr int kQ8Own = 2;
+// The same for a row of x of any type, of whole 16-byte vectors on 16-byte boundaries.
 bool q8_own_fits(const Q8Args& a);
 void launch_q8_own(const Q8Args& a, int tiles, int waves, unsigned grid, hipStream_t stream);
 void launch_q8_tile(const Q8Args& a, Q8Tile kind, unsigned grid, hipStream_t stream);

@@ -166,7 +166,6 @@ int fill_args(const gemv_ar_q8_plan* h, const int8_t* codes, const float* scales
   a->codes = codes;
   a->scales = scales;
   a->x = static_cast<const char*>(x);
-  a->ldx = ldx * elt_of(h->dtype);
   a->x_type = h->dtype;
   a->K = (int32_t)h->K;
   a->xq = xq;

@@ -49,37 +49,33 @@ struct Few {
 };
 
 template <int DT>
-__device__ __forceinline__ void round_rows(const Q8Args& a, const char* raw, int raw_pitch, int8_t* codes, float* scales, uint32_t* tops) {
+__device__ __forceinline__ void round_row(const Q8Args& a, const char* raw, int8_t* codes, float* scale_out, uint32_t* tops) {
   const int waves = blockDim.x >> 6, wave = threadIdx.x >> 6, units = (int)(a.pitch / 8);
-  for (int r = 0; r < (int)a.rows; ++r) {
-    uint32_t top = 0;
-    for (int u = threadIdx.x; u < units; u += blockDim.x) {
-      float f[8];
-      q8_load8<DT>(raw + r * raw_pitch, u * 8, a.K, f);
+  uint32_t top = 0;
+  for (int u = threadIdx.x; u < units; u += blockDim.x) {
+    float f[8];
+    q8_load8<DT>(raw, u * 8, a.K, f);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) top = q8_larger(top, __float_as_uint(f[i]) & 0x7fffffffu);
-    }
-    top = q8_largest(top);
-    if ((threadIdx.x & 63) == 0) tops[r * waves + wave] = top;
+    for (int i = 0; i < 8; ++i) top = q8_larger(top, __float_as_uint(f[i]) & 0x7fffffffu);
   }
+  top = q8_largest(top);
+  if ((threadIdx.x & 63) == 0) tops[wave] = top;
   __syncthreads();
-  for (int r = 0; r < (int)a.rows; ++r) {
-    uint32_t top = 0;
-    for (int w = 0; w < waves; ++w) top = q8_larger(top, tops[r * waves + w]);
-    const float scale = q8_scale(top);
-    if (threadIdx.x == 0) scales[r] = scale;
-    const Q8Rounder rounder(scale);
-    for (int u = threadIdx.x; u < units; u += blockDim.x) {
-      float f[8];
-      q8_load8<DT>(raw + r * raw_pitch, u * 8, a.K, f);
-      q8_store8(codes + r * a.pitch + u * 8, rounder, f);
-    }
+  top = 0;
+  for (int w = 0; w < waves; ++w) top = q8_larger(top, tops[w]);
+  const float scale = q8_scale(top);
+  if (threadIdx.x == 0) *scale_out = scale;
+  const Q8Rounder rounder(scale);
+  for (int u = threadIdx.x; u < units; u += blockDim.x) {
+    float f[8];
+    q8_load8<DT>(raw, u * 8, a.K, f);
+    q8_store8(codes + u * 8, rounder, f);
   }
   __syncthreads();
 }
 
-// OWN: the rows of x, two at most, are rounded here, by every workgroup for itself, while the first weights
-// are on their way: a launch less (one row x 4096 x 4096: 9.4 -> 6.5 us).  Eight waves, as they share the rounding (four: 6.8).
+// OWN: the one row of x is rounded here, by every workgroup for itself, while the first weights are on their way: a
+// launch less (x 4096 x 4096: 9.4 -> 6.5 us).  Eight waves, as they share the rounding (four: 6.8).
 template <int RT, int NT, int WW, int WAVES, bool OWN>
 __global__ __launch_bounds__(64 * WAVES) void q8_few_kernel(const Q8Args a) {
   typedef Few<RT, NT, WW, WAVES, OWN> F;
@@ -135,17 +131,16 @@ __global__ __launch_bounds__(64 * WAVES) void q8_few_kernel(const Q8Args a) {
     from[i] += ((lane & 7) ^ (row >> 1 & 7)) * 16;
     to[i] = lds0 + __builtin_amdgcn_readfirstlane(row - row8) * (int)kQ8Line;
   }
-  // OWN: behind the ring the rows' codes, then the rows as they are, in whole KiB, then their scales and the waves' largest.
+  // OWN: behind the ring the row's codes, then the row as it is, in whole KiB, then its scale and the waves' largest.
   char* codes = lds + F::LDS;
-  const int raw_bytes = OWN ? a.K * (a.x_type == EBAG_F32 ? 4 : 2) : 0, raw_pitch = (raw_bytes + 1023) / 1024 * 1024;
-  char* raw = codes + (OWN ? a.rows * a.pitch : 0);
-  float* own_scales = reinterpret_cast<float*>(raw + (OWN ? (int)a.rows : 0) * raw_pitch);
+  const int raw_bytes = OWN ? a.K * (a.x_type == EBAG_F32 ? 4 : 2) : 0, chunks = (raw_bytes + 1023) / 1024;
+  char* raw = codes + (OWN ? a.pitch : 0);
+  float* own_scale = reinterpret_cast<float*>(raw + chunks * 1024);
   if (OWN) {
-    const int chunks = raw_pitch / 1024;
-    for (int i = wave; i < (int)a.rows * chunks; i += WAVES) {
-      const int r = i / chunks, at = (i - r * chunks) * 1024 + lane * 16;
+    for (int i = wave; i < chunks; i += WAVES) {
+      const int at = i * 1024 + lane * 16;
       copy_to_lds((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)raw + i * 1024,
-                  reinterpret_cast<const int8_t*>(a.x + r * a.ldx + (at < raw_bytes ? at : raw_bytes - 16)));
+                  reinterpret_cast<const int8_t*>(a.x + (at < raw_bytes ? at : raw_bytes - 16)));
     }
   }
   const int lines = (int)(a.pitch / kQ8Line), steps = (lines + F::WK - 1) / F::WK, line0 = part * steps;
@@ -165,7 +160,7 @@ __global__ __launch_bounds__(64 * WAVES) void q8_few_kernel(const Q8Args a) {
   for (int b = 0; b < RT; ++b)
 #pragma unroll
     for (int t = 0; t < NT; ++t) sum[b][t] = i32x4{0, 0, 0, 0};
-  const char* own_x = codes + (r16 < (int)a.rows ? r16 : 0) * a.pitch + quarter * 16;
+  const char* own_x = codes + quarter * 16;
   auto multiply = [&](int stage, int line) __attribute__((always_inline)) {
     const char* rows = mine + stage * F::STAGE;
 #pragma unroll
@@ -189,14 +184,14 @@ __global__ __launch_bounds__(64 * WAVES) void q8_few_kernel(const Q8Args a) {
       arrived<(F::STAGES - 1) * F::COPIES>();
     else
       arrived<0>();
-    uint32_t* tops = reinterpret_cast<uint32_t*>(own_scales + kQ8Own);
+    uint32_t* tops = reinterpret_cast<uint32_t*>(own_scale + 1);
     int8_t* to_codes = reinterpret_cast<int8_t*>(codes);
     if (a.x_type == EBAG_F32)
-      round_rows<0>(a, raw, raw_pitch, to_codes, own_scales, tops);
+      round_row<0>(a, raw, to_codes, own_scale, tops);
     else if (a.x_type == EBAG_F16)
-      round_rows<1>(a, raw, raw_pitch, to_codes, own_scales, tops);
+      round_row<1>(a, raw, to_codes, own_scale, tops);
     else
-      round_rows<2>(a, raw, raw_pitch, to_codes, own_scales, tops);
+      round_row<2>(a, raw, to_codes, own_scale, tops);
   }
   int stage = 0;
   for (int step = 0; step < steps; ++step) {
@@ -243,7 +238,7 @@ __global__ __launch_bounds__(64 * WAVES) void q8_few_kernel(const Q8Args a) {
       for (int i = 0; i < 4; ++i) {
         const uint32_t n = first + 16 * t + 4 * quarter + i;
         if (n >= end) continue;
-        const float xs = OWN ? own_scales[n] : a.xs[q8_x_row(a, n)];
+        const float xs = OWN ? *own_scale : a.xs[q8_x_row(a, n)];
         float v = (float)sum[b][t][i] * (xs * ws);
         if (RT > 1 && pair == 2) {
           const float up = (float)sum[b + 1 < RT ? b + 1 : b][t][i] * (xs * wu);
@@ -260,9 +255,10 @@ void launch(const Q8Args& a, unsigned grid, hipStream_t stream) {
 }
 
 constexpr int kOwnWaves = 8;
+constexpr int64_t kOwnTiles = 1024;  // of 16 rows of weights
 int own_bytes(const Q8Args& a) {  // of LDS, behind the ring
   const int raw = a.K * (a.x_type == EBAG_F32 ? 4 : 2);
-  return (int)a.rows * ((int)a.pitch + (raw + 1023) / 1024 * 1024) + 4 * kQ8Own * (1 + kOwnWaves);
+  return (int)a.pitch + (raw + 1023) / 1024 * 1024 + 4 * (1 + kOwnWaves);
 }
 
 template <int RT, int WW>
@@ -291,10 +287,13 @@ void launch(const Q8Args& a, int x_tiles, int waves, unsigned grid, hipStream_t 
 
 }  // namespace
 
-// What the ring leaves of a CU's LDS, and x as copies take it.
+// What the ring leaves of a CU's LDS, and x as copies take it.  With more workgroups than are on the card at a time their
+// rounding costs more than the launch (bf16, in us, rounded here and first: 16384 x 4096 13.0, 17.3; 32768 x 160 10.0, 6.2; 32768
+// x 8192 56.9, 53.0; 65536 x 8192 107, 95); so does a second row (16384 x 4096 18.9, 17.9; 4096 x 8192 13.5, 12.1; 4096 x 4096
+// 8.8, 9.4).
 bool q8_own_fits(const Q8Args& a) {
   const int elt = a.x_type == EBAG_F32 ? 4 : 2;
-  return a.x && a.rows <= kQ8Own && !a.offsets && (int64_t)a.K * elt % 16 == 0 && a.ldx % 16 == 0 &&
+  return a.x && a.rows == 1 && !a.offsets && a.out_rows <= 16 * kOwnTiles && (int64_t)a.K * elt % 16 == 0 &&
          reinterpret_cast<uintptr_t>(a.x) % 16 == 0 && own_bytes(a) <= kCuLds - 64 * 1024;
 }
 
