@@ -227,9 +227,10 @@ __device__ __forceinline__ float top_of(const float* x) {
   return max_lanes(top, L);
 }
 
-// The k largest scores of a token.  MERGE (k up to 8): every lane sorts its keys and keeps
-// eight, and the lanes' lists become one in log2(L) merges, which every lane then has
-// whole.  Otherwise the largest of the lanes' first keys is taken off k times.
+// The k largest scores of a token.  K (8 or 16, k up to that): every lane sorts its keys and keeps
+// K, and the lanes' lists become one in log2(L) merges, which every lane then has
+// whole.  K = 0: the largest of the lanes' first keys is taken off k times (16384 tokens of 256 fp32 logits,
+// 16 choices, 21.4 us, in lists of sixteen 11.2).
 //
 // TOTALS: the probabilities are summed over a workgroup's tokens, in registers, then
 // over its waves in LDS, always in the same order; the choices are counted there
@@ -241,7 +242,7 @@ __device__ __forceinline__ float top_of(const float* x) {
 // of the time; sorting and merging take a third of them.  32 logits of a lane instead of 16 need fewer (two merges less for a token), but
 // half the waves hide less: 9.3 and 19.  Parts laid out for the second launch, 16 bytes of every workgroup for two columns, cost
 // the first more than they save there: 21.  With few tokens the chain is what counts: 32 tokens of 128 5.1 us.
-template <int V, int L, bool MERGE, bool TOTALS>
+template <int V, int L, int K, bool TOTALS>
 __global__ __launch_bounds__(TOTALS ? 1024 : 256) void choose_kernel(const ChooseArgs a) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
   const int lane = threadIdx.x % L, own = threadIdx.x / L, groups = blockDim.x / L;
@@ -297,8 +298,7 @@ __global__ __launch_bounds__(TOTALS ? 1024 : 256) void choose_kernel(const Choos
       const uint64_t some = __ballot(counted && lane == 0);
       if ((threadIdx.x & 63) == 0) atomicAdd(&counts[E], (int)__popcll(some));
     }
-    if constexpr (MERGE) {
-      constexpr int K = 8;
+    if constexpr (K > 0) {
       sort_down<K>(key);
       if constexpr (V > K) {
         sort_down<K>(key + K);
@@ -618,23 +618,25 @@ __global__ __launch_bounds__(256) void choose_backward_kernel(const ChooseArgs a
 typedef void (*choose_fn)(const ChooseArgs);
 
 // The instance for `lanes` lanes of `values` logits.
-template <bool TOTALS>
-choose_fn pick_forward(int values, int lanes, bool merge) {
-  if (values == 16) {
-    switch (lanes) {
-      case 4: return merge ? choose_kernel<16, 4, true, TOTALS> : choose_kernel<16, 4, false, TOTALS>;
-      case 8: return merge ? choose_kernel<16, 8, true, TOTALS> : choose_kernel<16, 8, false, TOTALS>;
-      case 16: return merge ? choose_kernel<16, 16, true, TOTALS> : choose_kernel<16, 16, false, TOTALS>;
-      default: return merge ? choose_kernel<16, 32, true, TOTALS> : choose_kernel<16, 32, false, TOTALS>;
-    }
-  }
-  if (values == 8) return choose_kernel<8, 64, false, TOTALS>;
+template <int K, bool TOTALS>
+choose_fn pick_wide(int lanes) {
   switch (lanes) {
-    case 4: return choose_kernel<4, 4, false, TOTALS>;
-    case 8: return choose_kernel<4, 8, false, TOTALS>;
-    case 16: return choose_kernel<4, 16, false, TOTALS>;
-    case 32: return choose_kernel<4, 32, false, TOTALS>;
-    default: return choose_kernel<4, 64, false, TOTALS>;
+    case 4: return choose_kernel<16, 4, K, TOTALS>;
+    case 8: return choose_kernel<16, 8, K, TOTALS>;
+    case 16: return choose_kernel<16, 16, K, TOTALS>;
+    default: return choose_kernel<16, 32, K, TOTALS>;
+  }
+}
+template <bool TOTALS>
+choose_fn pick_forward(int values, int lanes, int keep) {
+  if (values == 16) return keep == 8 ? pick_wide<8, TOTALS>(lanes) : keep == 16 ? pick_wide<16, TOTALS>(lanes) : pick_wide<0, TOTALS>(lanes);
+  if (values == 8) return choose_kernel<8, 64, 0, TOTALS>;
+  switch (lanes) {
+    case 4: return choose_kernel<4, 4, 0, TOTALS>;
+    case 8: return choose_kernel<4, 8, 0, TOTALS>;
+    case 16: return choose_kernel<4, 16, 0, TOTALS>;
+    case 32: return choose_kernel<4, 32, 0, TOTALS>;
+    default: return choose_kernel<4, 64, 0, TOTALS>;
   }
 }
 choose_fn pick_backward(int values, int lanes) {
@@ -660,19 +662,19 @@ int hipf(hipError_t e, const char* what) { return fail(EBAG_EHIP, "%s: %s", what
 
 // Lanes of a token and logits of a lane.  Four logits where there are few tokens, so that the steps are short and
 // spread over the card; 16, with fewer steps over the lanes, where the card is full with them.
-void shape_for(int64_t tokens, int E, int* values, int* lanes) {
+void shape_for(int64_t tokens, int E, int keep, int* values, int* lanes) {
   *lanes = 4;
   if (E > 32) {
     while (*lanes * 16 < E) *lanes *= 2;
     *values = 16;
-    if (tokens * *lanes >= 64 * 2048) return;
+    if (tokens * *lanes >= (keep == 16 ? 64 * 1024 : 64 * 2048)) return;
   }
   *values = E > 256 ? 8 : 4;
   while (*lanes * *values < E) *lanes *= 2;
 }
 
 int choose_args(ebag_a2a_moe_t h, const void* logits, int64_t ldl, int32_t dtype, int64_t tokens, const uint8_t* live,
-                int32_t normalise, ChooseArgs* a, int* values, int* lanes) {
+                int32_t normalise, int keep, ChooseArgs* a, int* values, int* lanes) {
   if (int rc = check_moe_plan(h, tokens)) return rc;
   if (dtype != EBAG_F32 && dtype != EBAG_F16 && dtype != EBAG_BF16) return fail(EBAG_EINVAL, "bad dtype %d", (int)dtype);
   if (normalise != 0 && normalise != 1) return fail(EBAG_EINVAL, "normalise must be 0 or 1");
@@ -694,7 +696,7 @@ int choose_args(ebag_a2a_moe_t h, const void* logits, int64_t ldl, int32_t dtype
   a->normalise = normalise;
   a->coef = (float)((double)h->experts / h->choices);
   a->turns = 1;
-  shape_for(tokens, a->E, values, lanes);
+  shape_for(tokens, a->E, keep, values, lanes);
   return EBAG_OK;
 }
 
@@ -711,7 +713,8 @@ int ebag_a2a_moe_choose(ebag_a2a_moe_t h, const void* logits, int64_t ldl, int32
                         int32_t* counts, float* sums, float* losses, float* work, hipStream_t stream) {
   ChooseArgs a;
   int values, lanes;
-  if (int rc = choose_args(h, logits, ldl, dtype, tokens, live, normalise, &a, &values, &lanes)) return rc;
+  const int keep = !h || h->choices <= 2 || h->choices > 16 ? 0 : h->choices <= 8 ? 8 : 16;
+  if (int rc = choose_args(h, logits, ldl, dtype, tokens, live, normalise, keep, &a, &values, &lanes)) return rc;
   if (tokens && (!ids || !weights)) return fail(EBAG_EINVAL, "null ids or weights");
   const bool totals = counts || sums || losses || work;
   if (totals && (!counts || !sums || !losses || !work))
@@ -738,8 +741,7 @@ int ebag_a2a_moe_choose(ebag_a2a_moe_t h, const void* logits, int64_t ldl, int32
   }
   size_t lds = (size_t)groups * a.k * 8;
   if (totals) lds += (size_t)(a.E + 1) * 4 * (1 + threads / 64) + 64;
-  const bool merge = a.k > 2 && a.k <= 8;
-  const choose_fn fn = totals ? pick_forward<true>(values, lanes, merge) : pick_forward<false>(values, lanes, merge);
+  const choose_fn fn = totals ? pick_forward<true>(values, lanes, keep) : pick_forward<false>(values, lanes, keep);
   hipLaunchKernelGGL(fn, dim3((unsigned)wgs), dim3(threads), lds, stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return hipf(e, "launch the choice");
@@ -756,7 +758,7 @@ int ebag_a2a_moe_choose_backward(ebag_a2a_moe_t h, const void* logits, int64_t l
                                  hipStream_t stream) {
   ChooseArgs a;
   int values, lanes;
-  if (int rc = choose_args(h, logits, ldl, dtype, tokens, live, normalise, &a, &values, &lanes)) return rc;
+  if (int rc = choose_args(h, logits, ldl, dtype, tokens, live, normalise, 0, &a, &values, &lanes)) return rc;
   if (!tokens) return EBAG_OK;
   if (!dlogits) return fail(EBAG_EINVAL, "null dlogits");
   if (dweights && !ids) return fail(EBAG_EINVAL, "null ids");

@@ -173,3 +173,18 @@ def test_more_tokens_than_one_launch_has_threads_for():
         x, y = logits[at:at + (1 << 28)].float(), out[at:at + (1 << 28)].float()
         assert bool(((x - y).abs() <= x.abs() * 2.0 ** -8).all())
     plan.close()
+
+
+@pytest.mark.parametrize("N,k,E,dtype,masked,few", [
+    (33000, 16, 60, "bfloat16", 0.0, 5), (17000, 9, 100, "float32", 0.9, 0), (8300, 12, 256, "float16", 0.0, 9), (4200, 16, 500, "float32", 0.3, 0),
+    (8300, 17, 250, "float32", 0.0, 0), (8300, 2, 250, "bfloat16", 0.0, 4), (70000, 11, 33, "float32", 0.0, 0)])
+def test_many_tokens_of_many_choices(N, k, E, dtype, masked, few):
+    import torch
+    from tests.test_gpu_choose import _logits
+    rng = np.random.default_rng([93, N, k, E])
+    plan = _plan(N, k, E)
+    logits = _logits(rng, N, E, dtype, masked, 2.0, few)
+    for normalise, totals in ((True, True), (False, False)):
+        call = Call(plan, logits, k, E, totals, normalise=normalise)
+        _check(call, logits, k, E, None, None, normalise)
+    plan.close()
