@@ -727,9 +727,11 @@ int ebag_a2a_moe_choose(ebag_a2a_moe_t h, const void* logits, int64_t ldl, int32
   a.sums = sums;
   a.losses = losses;
   a.work = work;
-  // With totals large workgroups, as every one of them leaves a part to be joined.
+  // With totals large workgroups, as every one of them leaves a part to be joined, but not so large that they leave CUs
+  // idle (with 512 and 1024 threads: 8192 tokens of 256, 8 choices 14.4 and 16.1 us, 7000 of 256, 12 choices 19.7 and 23.0;
+  // with 256, 512 and 1024: 4000 of 60 12.3, 10.0 and 10.1, 1000 of 256 16.0, 15.5 and 14.7).
   int threads = 256;
-  if (totals && tokens * lanes > 256 * 64) threads = 1024;
+  if (totals && tokens * lanes > 256 * 64) threads = tokens * lanes > kMostParts * 512 ? 1024 : 512;
   while (threads > 256 && threads / lanes * a.k > 6144) threads /= 2;  // 48 KiB of choices
   const int groups = threads / lanes;
   int64_t wgs = (tokens + groups - 1) / groups;
