@@ -224,7 +224,8 @@ void gemv_ar_q4_destroy(gemv_ar_q4_t h);
  *   experts: the same of row p with expert e's matrix,   offsets[e] <= p < offsets[e + 1]
  *
  * With glu = 1 the M rows are M / 2 gate rows and M / 2 up rows and the result
- * has M / 2 columns, y = silu(gate) * up, silu(v) = v / (1 + exp(-v)).
+ * has M / 2 columns, y = silu(gate) * up, silu(v) = v / (1 + exp(-v)), an fp32
+ * number: below 2^-126 (v from about -92 down) it has fewer than 24 bits.
  *
  * The sums are whole numbers and exact (K at most 2^17); each is rounded to fp32,
  * times the product of its scales, and once to y's type, the plan's or fp32.  Row r
