@@ -153,7 +153,8 @@ void gemv_ar_destroy(gemv_ar_t h);
  *   experts: y[p][m] = sum_k W[e][m][k] xrow(p)[k],          offsets[e] <= p < offsets[e + 1]
  *
  * With glu = 1 the M rows are M / 2 gate rows and M / 2 up rows and the result
- * has M / 2 columns, y = silu(gate) * up, silu(v) = v / (1 + exp(-v)).
+ * has M / 2 columns, y = silu(gate) * up, silu(v) = v / (1 + exp(-v)), an fp32
+ * number: below 2^-126 (v from about -92 down) it has fewer than 24 bits.
  *
  * x rows are K elements of dtype (EBAG_F32, EBAG_F16 or EBAG_BF16), row r at
  * element r * ldx; y rows are of dtype or fp32 (y_dtype), row r at element

@@ -28,12 +28,14 @@ def _cuda():
     torch.cuda.synchronize()
 
 
-def _check(got, g, u, y_dtype):
+def _check(got, g, u, y_dtype, off=4):
+    """off: how far g and u may be from the numbers themselves, in u."""
     import torch
     e = np.exp(-np.abs(g))
     act = g * np.where(g < 0, e, 1.0) / (1 + e)
     floor = (128 if y_dtype == "float32" else 1) * 2.0 ** -149
-    b = 1.01 * (np.abs(act) * (2 * np.abs(g) + 10) * 2.0 ** -22 + floor) * np.abs(u) + 5 * U * np.abs(act * u) + 2.0 ** -149
+    rel = (np.abs(g) + 8) * 2.0 ** -22 + (np.abs(g) + 2) * off * U
+    b = 1.01 * (np.abs(act) * rel + floor) * np.abs(u) + (off + 1) * U * np.abs(act * u) + 2.0 ** -149
     want = act * u
     got = got.double().cpu().numpy()
     lo, hi = (torch.from_numpy(v).to(getattr(torch, y_dtype)).double().numpy() for v in (want - b, want + b))
@@ -71,4 +73,38 @@ def test_gates_in_8_bits(rows, experts, dtype):
             ends = torch.tensor([0, rows // 3, rows // 3, rows], dtype=torch.int32, device="cuda")
             plan.experts(codes, scales, x, ends, y, xq, xs)
         _check(y, z[:, :H], z[:, H:], y_dtype)
+    plan.close()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,experts", [(1, 1), (5, 1), (40, 1), (1000, 1), (900, 3)])
+def test_gates_in_4_bits(rows, experts, dtype):
+    """One column of x is not zero, and its weight 7 times the scale.  A sum is made of that term with a part of up to 143 s |x| that
+    comes off again: four roundings of 286 s |x| 2^-23, of 7 s |x| less than 330 u."""
+    import torch
+    import paper_2305_06942_amd as ebag
+    rng = np.random.default_rng([112, rows, experts])
+    K = 32
+    most = 1e3 if dtype == "float16" else 1e30
+    gates = GATES[(np.abs(GATES) <= most) & ((np.abs(GATES) >= 1e-3) | (dtype != "float16"))]
+    gates, ups = np.repeat(gates, 4), np.tile([1.0, -3e-2, 1e4, most], len(gates))
+    H = len(gates)
+    plan = ebag.Q4Gemv(2 * H, K, K, TYPES.index(dtype), experts=experts, glu=1)
+    codes = torch.from_numpy(rng.integers(0, 256, size=(experts, 2 * H, K // 2), dtype=np.uint8)).cuda()
+    sign = np.sign(np.concatenate((gates, ups)))
+    codes[:, :, 0] = torch.from_numpy((8 + 7 * sign).astype(np.uint8)).cuda()
+    scales = torch.from_numpy(np.abs(np.concatenate((gates, ups))) / 7).to(getattr(torch, dtype)).cuda()
+    x = torch.zeros((rows, K), dtype=scales.dtype, device="cuda")
+    x[:, 0] = torch.from_numpy(rng.choice([1.0, 1.0, 0.5, 0.96875, 0.25], size=rows))
+    x[rows - 1, 0] = 1
+    z = x[:, :1].double().cpu().numpy() * (7 * sign * scales.double().cpu().numpy())[None]
+    weights = codes, scales.expand(experts, -1).contiguous(), None
+    for y_dtype in {dtype, "float32"}:
+        y = torch.full((rows, H), float("nan"), dtype=getattr(torch, y_dtype), device="cuda")
+        if experts == 1:
+            plan.forward(*weights, x, y)
+        else:
+            ends = torch.tensor([0, rows // 3, rows // 3, rows], dtype=torch.int32, device="cuda")
+            plan.experts(*weights, x, ends, y)
+        _check(y, z[:, :H], z[:, H:], y_dtype, 330)
     plan.close()
