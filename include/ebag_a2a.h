@@ -460,8 +460,9 @@ int ebag_a2a_moe_combine_backward(ebag_a2a_moe_t h, const void* dout, int64_t ld
  * p[n][e] of its expert; with 1 the softmax over the chosen experts' logits alone.
  *
  *   T          tokens that count: live[n] is not 0 (NULL: all) and a logit of
- *              theirs is above -inf.  The others have choices of -1 and weights
- *              of 0, and logits of tokens that are not live are not read
+ *              theirs is above -inf, which NaN is not.  The others have choices
+ *              of -1 and weights of 0, and logits of tokens that are not live are
+ *              not read
  *   counts[e]  choices of expert e; counts[experts] = T
  *   sums[e]    sum over them of p[n][e]; sums[experts] the sum of z[n]^2, z the
  *              logarithm of the sum of l[n]'s exponentials
@@ -473,10 +474,12 @@ int ebag_a2a_moe_combine_backward(ebag_a2a_moe_t h, const void* dout, int64_t ld
  * give the gradient of the loss over all their tokens.
  *
  * Logits are fp32, fp16 or bf16, row n at element n * ldl, aligned to the element
- * only; all else is computed in fp32.  A NaN or +inf logit makes its own token's
- * probabilities NaN, and with them its weights, unless normalise is 1 and it is
- * not chosen, the totals, and its row of the gradient.  Results are the same bits
- * on every run.  Outputs must not overlap inputs.
+ * only; all else is computed in fp32.  A NaN or +inf logit makes the probabilities of its
+ * own token, where that counts, NaN, and with them its weights, unless normalise is 1 and
+ * it is not chosen, the totals, and its row of the gradient.  A token of nothing but NaN
+ * and -inf does not count: it leaves no NaN anywhere, its row of the gradient is
+ * zeros, and what shows it is a T below the number of live tokens.  Results are the same
+ * bits on every run.  Outputs must not overlap inputs.
  */
 
 /* fp32 elements of `work` that a call with totals needs, for any number of tokens. */

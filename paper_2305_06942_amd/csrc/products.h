@@ -61,8 +61,8 @@ inline int64_t most_tiles(int64_t rows, int64_t experts, int64_t cols) {
 
 // v / (1 + exp(-v)).  With the short exponential, off by (|v| + 8) 2^-22, where y is rounded
 // to 16 bits, in two parts below -64, as exp(-v) would overflow where bf16 still holds the
-// result (32768 rows on 64 gated experts of 4096 x 2048 in 4 bits 776 -> 784 us); an fp32 y gets the full one, of -|v|, which does not overflow where the
-// result is still a number.
+// result (32768 rows on 64 gated experts of 4096 x 2048 in 4 bits 776 -> 784 us); an fp32 y
+// gets the full one, of -|v|, which does not overflow where the result is still a number.
 template <bool Y32>
 __device__ __forceinline__ float silu(float v) {
   if (!Y32) return v / (1.f + __expf(-__builtin_fmaxf(v, -64.f))) * __expf(__builtin_fminf(v + 64.f, 0.f));
