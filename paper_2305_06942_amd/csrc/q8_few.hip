@@ -17,9 +17,10 @@ constexpr int kCuLds = 160 * 1024;
 
 // 16 bytes of each lane from memory into LDS, `to` and behind, without a register between: the wave may have as many
 // under way as there is LDS for them.  The compiler's own builtin would have every later load from LDS wait for all of
-// them; here the kernel waits itself (arrived()), by their number, as they arrive in order.
+// them; here the kernel waits itself (arrived()), by their number, as they arrive in order.  The LDS address goes in m0, as an
+// operand, so that the compiler knows of it; the s_nop is the wait state behind its write.
 __device__ __forceinline__ void copy_to_lds(uint32_t to, const int8_t* from) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory");
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"{m0}"(to), "v"(from) : "memory");
 }
 // Waits until at most N copies of this wave are under way, and for the other waves to have come as far.
 template <int N>
