@@ -240,7 +240,9 @@ typedef struct gemv_ar_q8_plan* gemv_ar_q8_t;
  * rows (below 2^31) and K columns (1..2^17), glu 0 or 1 (M even).  It owns no device
  * memory; its calls share nothing but the xq and xs that the caller gives to several,
  * may run on any stream and can be captured into a graph.  They must be made with the
- * plan's device current (EBAG_EINVAL otherwise). */
+ * plan's device current (EBAG_EINVAL otherwise).  With M up to 2^30 every product
+ * that the card's memory holds has a launch; above, one of too many tiles is refused
+ * (EBAG_EUNSUPPORTED) before anything is launched. */
 int gemv_ar_q8_create(gemv_ar_q8_t* out, int64_t M, int64_t K, int32_t dtype, int32_t experts, int32_t glu);
 
 /* Bytes of a row of codes and of xq. */

@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "tiles.h"
+
 namespace ebag {
 
 // Which rows of y, and whose matrix, slot number `slot` of tiles of `cols` rows
@@ -50,13 +52,6 @@ __device__ __forceinline__ bool find_tile(const Args& a, uint32_t slot, uint32_t
     before += __shfl(upto, 63);
   }
   return false;
-}
-
-// Most tiles of `cols` rows that `rows` rows of `experts` experts and the
-// dropped rows behind them can make.
-inline int64_t most_tiles(int64_t rows, int64_t experts, int64_t cols) {
-  const int64_t n = (rows + (experts + 1) * (cols - 1)) / cols;
-  return n < rows ? n : rows;
 }
 
 // v / (1 + exp(-v)).  With the short exponential, off by (|v| + 8) 2^-22, where y is rounded

@@ -7,18 +7,13 @@
 #include "common.h"
 #include "lanes.h"
 #include "products.h"
+#include "q8_choose.h"
 #include "vec16.h"
 
 namespace ebag {
 
 typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 typedef int32_t i32x16 __attribute__((ext_vector_type(16)));
-
-// Bytes of a row of codes: whole cache lines, so that rows begin on one and every
-// step of a product is whole.  Rows of x end in zeros, so what stands behind a
-// row of weights does not matter.
-constexpr int64_t kQ8Line = 128;
-constexpr int64_t q8_pitch(int64_t K) { return (K + kQ8Line - 1) / kQ8Line * kQ8Line; }
 
 struct Q8Args {
   const int8_t* codes;
@@ -170,11 +165,6 @@ __device__ __forceinline__ float q8_silu(float v) {
   const float h = __builtin_amdgcn_exp2f(0.72134752f * __builtin_fminf(v, 20.f));  // 1 / (2 ln 2)
   return v * (h * __builtin_amdgcn_rcpf(__builtin_fmaf(h, h, 1.f))) * h;
 }
-
-// Rows of weights and rows of x of a workgroup of the matrix-product kernel.
-enum Q8Tile { Q8_256x64, Q8_512x128, Q8_256x256 };
-constexpr int q8_tile_w(Q8Tile t) { return t == Q8_512x128 ? 512 : 256; }
-constexpr int q8_tile_x(Q8Tile t) { return t == Q8_256x64 ? 64 : t == Q8_512x128 ? 128 : 256; }
 
 // tiles: of 16 rows of weights of a wave; x_tiles: of 16 rows of x; waves: of four, that have different rows of weights.
 void launch_q8_few(const Q8Args& a, int tiles, int x_tiles, int waves, unsigned grid, hipStream_t stream);

@@ -3,7 +3,6 @@
 #include <hip/hip_runtime.h>
 
 #include <climits>
-#include <cmath>
 #include <new>
 
 #include "ebag_a2a.h"
@@ -184,108 +183,44 @@ int fill_args(const gemv_ar_q8_plan* h, const int8_t* codes, const float* scales
   return EBAG_OK;
 }
 
-// Waves with different rows of weights: as many as leave every CU a workgroup, since they share x; the others share the
-// columns (bf16, in us by 1, 2, 4 and 8 of them: 16 rows x 4096 x 4096 6.7, 7.7; x 14336 x 4096 16.8, 13.1; x 65536 x 8192
-// 103, 92; 32 rows 8.0, 10.0, 12.7; 20.6, 15.2, 14.7; 135, 104, 95; 64 rows 11.3, 12.7, 17.5, 20.3; 40, 20.3, 19.4, 22.2;
-// 238, 136, 109, 97).  One tile of weights to a wave; two, for glu, take 1 to 30 % longer.  Where few workgroups have
-// much of K each, eight waves share it.
-int launch_few(Q8Args a, int x_tiles, hipStream_t stream) {
-  const int cols = 16 * x_tiles;
-  const int64_t slots = a.offsets ? most_tiles(a.rows, a.experts, cols) : (a.rows + cols - 1) / cols;
-  const int64_t wave_tiles = (a.out_rows + 15) / 16, used = a.offsets ? (a.rows + cols - 1) / cols : slots;
-  const int most = x_tiles == 1 ? 2 : x_tiles == 2 ? 4 : 8;
-  int waves = x_tiles == 8 ? 4 : 1;
-  const int64_t lines = a.pitch / kQ8Line;  // not more waves to the columns than lines (77 rows x 2610 x 94, 17 experts: 44 -> 10 us)
-  while (waves < most && (wave_tiles * used >= 200 * 2 * waves || lines * waves < 4)) waves *= 2;
-  // A few tiles are not an eighth for each XCD: they are left to all of them (2920 rows x 54 x 2587: 15.3 -> 7.7 us).
-  const int64_t grid_tiles = (wave_tiles + waves - 1) / waves;
-  a.spread = grid_tiles < 64 ? 0 : 3;
-  const int64_t eighths = ((grid_tiles - 1) >> a.spread) + 1;
-  const int64_t group = !a.spread ? 1 : a.offsets ? (a.rows > (int64_t)cols * a.experts ? 4 : 1) : slots < 8 ? slots : 8, groups = (slots + group - 1) / group;
-  const int64_t grid = (eighths << a.spread) * group * groups;
-  if (grid > UINT32_MAX / 512) return fail(EBAG_EUNSUPPORTED, "too many tiles for one launch");
-  a.by_tiles = make_divisor(eighths);
-  a.tiles = (uint32_t)grid_tiles;
-  a.by_group = make_divisor(group);
+Q8Call call_of(const Q8Args& a) {
+  return Q8Call{a.M, a.out_rows, a.pitch, a.rows, a.experts, a.offsets != nullptr, a.glu != 0};
+}
+
+void launch_few(Q8Args a, const Q8Shape& s, int x_tiles, hipStream_t stream) {
+  a.by_tiles = make_divisor(s.tiles);
+  a.spread = s.spread;
+  a.tiles = (uint32_t)s.all_tiles;
+  a.by_group = make_divisor(s.group);
   if (a.x)
-    launch_q8_own(a, a.glu ? 2 : 1, waves, (unsigned)grid, stream);
+    launch_q8_own(a, a.glu ? 2 : 1, s.waves, (unsigned)s.grid, stream);
   else
-    launch_q8_few(a, a.glu ? 2 : 1, x_tiles, waves, (unsigned)grid, stream);
+    launch_q8_few(a, a.glu ? 2 : 1, x_tiles, s.waves, (unsigned)s.grid, stream);
+}
+
+void launch_tile(Q8Args a, const Q8Shape& s, Q8Tile kind, hipStream_t stream) {
+  a.by_tiles = make_divisor(s.tiles);
+  a.whole = (uint32_t)(s.grid / 256 * 256);
+  launch_q8_tile(a, kind, (unsigned)s.grid, stream);
+}
+
+// The product, its rows rounded first where x is given and the product does not do that itself.  The kernel is chosen
+// before anything is launched.
+int multiply(const gemv_ar_q8_plan* h, Q8Args a, int64_t ldx, int8_t* xq, float* xs, hipStream_t stream) {
+  const Q8Call call = call_of(a);
+  if (q8_own_fits(a)) {
+    launch_few(a, q8_few_shape(call, 1, true), 1, stream);
+  } else {
+    const Q8Kernel* k = q8_choose(call);
+    if (!k) return fail(EBAG_EUNSUPPORTED, "too many tiles for one launch: M=%lld, rows=%u", (long long)a.M, a.rows);
+    if (a.x)
+      if (int rc = launch_round(h, a.x, ldx, a.x_rows, xq, xs, stream)) return rc;
+    a.x = nullptr;
+    const Q8Shape s = q8_shape(call, *k);
+    k->x_tiles ? launch_few(a, s, k->x_tiles, stream) : launch_tile(a, s, k->tile, stream);
+  }
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? EBAG_OK : hipf(e, "launch the product in 8 bits");
-}
-
-int launch_tile(Q8Args a, Q8Tile kind, hipStream_t stream) {
-  const int x_rows = q8_tile_x(kind);
-  const int64_t per_wg = q8_tile_w(kind) / (a.glu ? 2 : 1), tiles = (a.out_rows + per_wg - 1) / per_wg;
-  const int64_t slots = a.offsets ? most_tiles(a.rows, a.experts, x_rows) : (a.rows + x_rows - 1) / x_rows;
-  const int64_t grid = (slots + 3) / 4 * 4 * tiles;
-  if (grid > UINT32_MAX / 512) return fail(EBAG_EUNSUPPORTED, "too many tiles for one launch");
-  a.by_tiles = make_divisor(tiles);
-  a.whole = (uint32_t)(grid / 256 * 256);
-  launch_q8_tile(a, kind, (unsigned)grid, stream);
-  const hipError_t e = hipGetLastError();
-  return e == hipSuccess ? EBAG_OK : hipf(e, "launch the product in 8 bits");
-}
-
-// Which kernel, by a model of measured times in us.  A kernel has `cols` rows of x and `rows` of weights to a workgroup.
-// `fix` is its beginning and end; K = 4096 (times K / 4096 for others) takes at least `least`, a workgroup's own time, and
-// otherwise `start` and `each` ns for every 16 x 16 sums, or `round` for every 256 workgroups of the largest tiles, one
-// to a CU.  With a shorter K the results' own time shows, `ends` ns for 16 x 16 of them, and the largest tiles take at
-// least `floor`.  Where the weights are more than the caches hold, memory's rate bounds all of them, `rate` in TB/s, at 1.5 times
-// the bytes with two tiles of x and so on in the kernel that streams (its tiles of x share weights in the L2 by half).
-// Fitted to 129 products in bf16 with every kernel, K from 80 to 10128: what it takes is 1 % slower than the fastest of the
-// seven on average, 33 % at most.  Some of them, in us by 16, 32, 64 and 128 rows of x in the streaming kernel, 256 x 64,
-// 512 x 128 and 256 x 256:
-//   4096 x 4096: 64 rows 9.5, 9.9, 11.5, 24, 20.3, 48, 45; 256 rows 25, 16.7, 18.3, 27, 21, 50, 48; 512 rows 45, 30.5, 20, 28.5, 22.7,
-//     50, 48; 2048 rows 167, 88, 56, 63, 41, 56, 52
-//   128 rows x 65536 x 8192: 354, 206, 143, 120, 194, 215, 347; 512 rows x 20000 x 256: 56, 27, 21, 30, 14, 18, 27
-//   2920 rows x 54 x 2587: 7.7, 10.4, 11.8, 20, 17, 44, 42
-//   gated experts of 2 x 1024 x 2048: 128 of them with 2 rows each 85, 88, 214, 140, 85, 98, 133; 64 with 32 rows each 88, 62,
-//     65, 88, 53, 58, 74; of 2 x 2048 x 2048, 64 with 512 rows each 1724, 850, 648, 568, 387, 377, 384
-struct Kernel {
-  int x_tiles;  // of 16 rows, in the streaming kernel; 0: the matrix-product kernel
-  Q8Tile tile;
-  double cols, rows, fix, floor, least, start, each, ends, round, rate;
-};
-constexpr Kernel kKernels[] = {
-    {1, Q8_256x64, 16, 16, 3.1, 0, 3.6, 1, 4.4, 1.7, 0, 5.6},      {2, Q8_256x64, 32, 16, 3.9, 0, 3.3, 4.1, 2.1, 0.5, 0, 5.6},
-    {4, Q8_256x64, 64, 16, 5.2, 0, 4.8, 4.3, 1.9, 0.3, 0, 5.6},    {8, Q8_256x64, 128, 16, 4.9, 0, 22, 0, 1.6, 0.45, 0, 4.5},
-    {0, Q8_256x64, 64, 256, 5.3, 0, 18, 2.5, 0.9, 0.18, 0, 5.4},   {0, Q8_512x128, 128, 512, 4.2, 17, 42, 0, 0, 0.3, 58, 2.5},
-    {0, Q8_256x256, 256, 256, 7.5, 14, 43, 0, 0, 0.25, 50, 1.5}};
-
-double time_of(const Kernel& k, const Q8Args& a) {
-  const double M = (double)a.M, scale = (double)a.pitch / 4096;
-  const double used = a.offsets ? (a.rows < (uint32_t)a.experts ? a.rows : a.experts) : 1;  // matrices with rows
-  const double per = (double)a.rows / used;
-  // Tiles of x: an expert's last one is half full on average.
-  double slots = a.offsets ? a.rows / k.cols + used / 2 : std::ceil(a.rows / k.cols);
-  slots = slots < used ? used : slots;
-  const double wgs = std::ceil(M / k.rows) * slots, sums = std::ceil(M / k.rows) * (k.rows / 16) * slots * (k.cols / 16);
-  double t = k.round ? std::ceil(wgs / 256) * k.round : k.start + sums * k.each * 1e-3;
-  t = k.fix + scale * (t < k.least ? k.least : t);
-  if (scale < 1) t += sums * k.ends * 1e-3 * (1 - scale);
-  if (t < k.floor) t = k.floor;
-  const double bytes = used * M * (double)a.pitch;
-  if (bytes > 128e6) {
-    double memory = bytes / (k.rate * 1e6);
-    if (k.x_tiles) memory *= (1 + 0.5 * (std::ceil(per / k.cols) - 1)) * (a.offsets && k.x_tiles > 1 ? 1.25 : 1);
-    // One workgroup on a CU, or two that share weights, have too few loads under way.
-    if (!k.x_tiles && !k.round && (wgs < 512 || (!a.offsets && per > k.cols))) memory *= 2;
-    if (memory > t) t = memory;
-  }
-  return t;
-}
-
-int launch(const Q8Args& a, hipStream_t stream) {
-  if (a.x) return launch_few(a, 1, stream);
-  const Kernel* best = nullptr;
-  double least = 0;
-  for (const Kernel& k : kKernels) {
-    const double t = time_of(k, a);
-    if (!best || t < least) best = &k, least = t;
-  }
-  return best->x_tiles ? launch_few(a, best->x_tiles, stream) : launch_tile(a, best->tile, stream);
 }
 
 }  // namespace
@@ -346,12 +281,7 @@ int gemv_ar_q8_forward(gemv_ar_q8_t h, const int8_t* codes, const float* scales,
   if (!rows) return EBAG_OK;
   Q8Args a;
   if (int rc = fill_args(h, codes, scales, x, ldx, rows, xq, xs, rows, y, ldy, y_dtype, &a)) return rc;
-  if (!q8_own_fits(a)) {
-    if (x)
-      if (int rc = launch_round(h, x, ldx, rows, xq, xs, stream)) return rc;
-    a.x = nullptr;
-  }
-  return launch(a, stream);
+  return multiply(h, a, ldx, xq, xs, stream);
 }
 
 int gemv_ar_q8_experts(gemv_ar_q8_t h, const int8_t* codes, const float* scales, const void* x, int64_t ldx, int64_t x_rows,
@@ -369,10 +299,7 @@ int gemv_ar_q8_experts(gemv_ar_q8_t h, const int8_t* codes, const float* scales,
   a.offsets = offsets;
   a.src = src;
   a.by_choices = make_divisor(src ? choices : 1);
-  a.x = nullptr;
-  if (x)
-    if (int rc = launch_round(h, x, ldx, x_rows, xq, xs, stream)) return rc;
-  return launch(a, stream);
+  return multiply(h, a, ldx, xq, xs, stream);
 }
 
 void gemv_ar_q8_destroy(gemv_ar_q8_t h) { delete h; }

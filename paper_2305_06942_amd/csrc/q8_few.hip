@@ -255,16 +255,15 @@ void launch(const Q8Args& a, unsigned grid, hipStream_t stream) {
   hipLaunchKernelGGL((q8_few_kernel<RT, NT, WW, WAVES, false>), dim3(grid), dim3(64 * WAVES), (Few<RT, NT, WW, WAVES, false>::LDS), stream, a);
 }
 
-constexpr int kOwnWaves = 8;
 constexpr int64_t kOwnTiles = 1024;  // of 16 rows of weights
 int own_bytes(const Q8Args& a) {  // of LDS, behind the ring
   const int raw = a.K * (a.x_type == EBAG_F32 ? 4 : 2);
-  return (int)a.pitch + (raw + 1023) / 1024 * 1024 + 4 * (1 + kOwnWaves);
+  return (int)a.pitch + (raw + 1023) / 1024 * 1024 + 4 * (1 + kQ8OwnWaves);
 }
 
 template <int RT, int WW>
 void launch_own(const Q8Args& a, unsigned grid, hipStream_t stream) {
-  constexpr int WAVES = kOwnWaves / RT;
+  constexpr int WAVES = kQ8OwnWaves / RT;
   hipLaunchKernelGGL((q8_few_kernel<RT, 1, WW, WAVES, true>), dim3(grid), dim3(64 * WAVES), (Few<RT, 1, WW, WAVES, true>::LDS) + own_bytes(a),
                      stream, a);
 }
