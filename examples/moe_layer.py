@@ -49,9 +49,17 @@ class Order:
         self.plan.sort(expert_of, offsets, pos, src)
         return offsets, pos, src
 
+    @staticmethod
+    def readable(logits):
+        """Logits as the library's router takes them: of other types as float32, and with rows of adjacent columns that do not
+        overlap."""
+        if logits.dtype not in (torch.float32, torch.float16, torch.bfloat16):
+            logits = logits.float()
+        return logits if logits.stride(1) == 1 and logits.stride(0) >= logits.shape[1] else logits.contiguous()
 
     def choose(self, logits):
         """(experts int32, weights float32) [tokens, choices]; a token's weights add up to 1."""
+        logits = self.readable(logits)
         shape = (logits.shape[0], self.choices)
         ids = torch.empty(shape, dtype=torch.int32, device=logits.device)
         weights = torch.empty(shape, dtype=torch.float32, device=logits.device)
@@ -187,7 +195,7 @@ class TrainingLayer(torch.nn.Module):
     def with_losses(self, x, logits, live=None):
         """(the layer's output, float32 [2]: the balance loss and the mean square of the logits' log-sum).  live: which
         tokens of a padded batch count; the others' rows of the output are zeros."""
-        expert_of, weights, losses = _Choose.apply(logits.contiguous(), self.order.plan, live)
+        expert_of, weights, losses = _Choose.apply(self.order.readable(logits).contiguous(), self.order.plan, live)
         offsets, pos, _ = self.order.sort(expert_of)
         xs = _Dispatch.apply(x, self.order.plan, offsets, pos)
         ends = offsets.tolist()
