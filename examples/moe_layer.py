@@ -133,17 +133,17 @@ class _Choose(torch.autograd.Function):
         ids, counts = new(n, k, dtype=torch.int32), new(experts + 1, dtype=torch.int32)
         weights, losses = new(n, k), new(2)
         plan.choose(logits, ids, weights, counts, new(experts + 1), losses, new(plan.choose_work), live=live)
-        ctx.plan, ctx.live = plan, live
-        ctx.save_for_backward(logits, ids, counts)
+        ctx.plan = plan
+        ctx.save_for_backward(logits, ids, counts, live)
         ctx.mark_non_differentiable(ids)
         return ids, weights, losses
 
     @staticmethod
     @once_differentiable
     def backward(ctx, _, dweights, dlosses):
-        logits, ids, counts = ctx.saved_tensors
+        logits, ids, counts, live = ctx.saved_tensors
         dlogits = torch.empty_like(logits)
-        ctx.plan.choose_backward(logits, ids, dweights.contiguous(), dlogits, counts=counts, dlosses=dlosses.contiguous(), live=ctx.live)
+        ctx.plan.choose_backward(logits, ids, dweights.contiguous(), dlogits, counts=counts, dlosses=dlosses.contiguous(), live=live)
         return dlogits, None, None
 
 

@@ -64,3 +64,19 @@ def test_training(example):
     leaf = logits[:1].detach().requires_grad_()
     layer(x, leaf.expand(37, -1)).sum().backward()
     assert leaf.grad.isfinite().all()
+
+
+@pytest.mark.parametrize("what", ["live", "logits"])
+def test_what_the_gradient_needs_is_not_changed_in_between(example, what):
+    """autograd refuses the backward pass of a call whose mask or logits were written to since."""
+    import torch
+    gate_up, down, x, logits = example.make(20, 6, 2, 64, 32, dtype=torch.float32)
+    layer = example.TrainingLayer(gate_up, down, 2, 20)
+    leaf = logits.requires_grad_()
+    live = torch.arange(20, device="cuda") % 3 > 0
+    out, losses = layer.with_losses(x, leaf, live)
+    (out.sum() + losses.sum()).backward(retain_graph=True)
+    with torch.no_grad():
+        {"live": live, "logits": leaf}[what].zero_()
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        (out.sum() + losses.sum()).backward()
