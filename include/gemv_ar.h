@@ -229,7 +229,9 @@ void gemv_ar_q4_destroy(gemv_ar_q4_t h);
  * number: below 2^-126 (v from about -92 down) it has fewer than 24 bits.
  *
  * The sums are whole numbers and exact (K at most 2^17); each is rounded to fp32,
- * times the product of its scales, and once to y's type, the plan's or fp32.  Row r
+ * times the product of its scales, and once to y's type, the plan's or fp32.  That product is an
+ * fp32 number, too: scales that multiply to less than 2^-126 have fewer than its 24
+ * bits, from 2^128 on they are an infinity (and with a sum of 0 a NaN).  Row r
  * of x starts at element r * ldx, of y at element r * ldy; neither needs an alignment
  * beyond its elements'; codes and xq are 16-byte aligned.  Outputs must not overlap inputs.
  * A row's results are the same bits on every run and whatever rows are with it.
