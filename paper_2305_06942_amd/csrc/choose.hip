@@ -661,7 +661,17 @@ choose_fn pick_backward(int values, int lanes) {
 int hipf(hipError_t e, const char* what) { return fail(EBAG_EHIP, "%s: %s", what, hipGetErrorString(e)); }
 
 // Lanes of a token and logits of a lane.  Four logits where there are few tokens, so that the steps are short and
-// spread over the card; 16, with fewer steps over the lanes, where the card is full with them.
+// spread over the card; 16, with fewer steps over the lanes, where the card is full with them.  fp32 with totals, in us
+// by four (eight above 256 experts) and by 16:
+//   8 choices: 16384 tokens of 64 11.7, 11.4; 32768 of 64 16.3, 12.7; 8192 of 128 13.4, 12.0; 16384 of 128 18.7, 13.3; 4096 of 256
+//     14.2, 12.6; 8192 of 256 20.1, 13.6; 2048 of 512 15.2, 14.0; 4096 of 512 17.7, 15.1
+//   16 choices: 8192 of 64 11.7, 14.9; 16384 of 64 14.0, 14.7; 4096 of 128 13.2, 15.5; 8192 of 128 16.4, 14.8; 2048 of 256 14.2, 15.9;
+//     4096 of 256 17.5, 14.5; 1024 of 512 17.0, 17.5; 2048 of 512 18.4, 16.5
+//   2 choices: 16384 of 64 10.1, 12.1; 65536 of 64 18.0, 18.2; 8192 of 128 11.6, 13.2; 32768 of 128 20.3, 19.6; 4096 of 256
+//     12.1, 13.4; 8192 of 256 15.1, 14.9; 4096 of 512 14.9, 16.3
+//   the gradient: 32768 of 64 6.4, 9.0; 8192 of 128 4.7, 5.3; 16384 of 128 6.7, 6.7; 8192 of 256 6.9, 7.3; 16384 of 256 11.1, 10.9;
+//     4096 of 512 6.7, 7.2; 8192 of 512 10.6, 10.9
+// Up to 32 experts 16 logits would leave lanes idle: 16384 of 32 with 2 choices 8.3, 12.6; 65536 of 32 11.2, 15.7, with 8 14.4, 14.3.
 void shape_for(int64_t tokens, int E, int keep, int* values, int* lanes) {
   *lanes = 4;
   if (E > 32) {
@@ -713,6 +723,10 @@ int ebag_a2a_moe_choose(ebag_a2a_moe_t h, const void* logits, int64_t ldl, int32
                         int32_t* counts, float* sums, float* losses, float* work, hipStream_t stream) {
   ChooseArgs a;
   int values, lanes;
+  // Lists of eight or sixteen, or the largest taken off k times, where that is once or twice (fp32, in us by lists of eight and
+  // taken off: 16384 tokens of 256, one choice 8.0, 7.6, with totals 17.0, 18.8; two 7.6, 8.1, 16.8, 19.5; three 7.6, 9.2, 16.9, 20.6;
+  // eight 7.7, 14.1, 17.0, 24.3; 32768 of 64, one choice 4.8, 4.9, with totals 12.1, 13.2; two 4.8, 5.4, 12.0, 13.6): one and two
+  // choices with totals lose 8 to 14 % by this rule.
   const int keep = !h || h->choices <= 2 || h->choices > 16 ? 0 : h->choices <= 8 ? 8 : 16;
   if (int rc = choose_args(h, logits, ldl, dtype, tokens, live, normalise, keep, &a, &values, &lanes)) return rc;
   if (tokens && (!ids || !weights)) return fail(EBAG_EINVAL, "null ids or weights");
@@ -728,8 +742,9 @@ int ebag_a2a_moe_choose(ebag_a2a_moe_t h, const void* logits, int64_t ldl, int32
   a.losses = losses;
   a.work = work;
   // With totals large workgroups, as every one of them leaves a part to be joined, but not so large that they leave CUs
-  // idle (with 512 and 1024 threads: 8192 tokens of 256, 8 choices 14.4 and 16.1 us, 7000 of 256, 12 choices 19.7 and 23.0;
-  // with 256, 512 and 1024: 4000 of 60 12.3, 10.0 and 10.1, 1000 of 256 16.0, 15.5 and 14.7).
+  // idle (8 choices, with 256, 512 and 1024 threads: 500 tokens of 256 15.0, 12.6 and 13.1 us, 1000 15.8, 15.0 and 14.6, 2000 18.8, 16.1
+  // and 16.7, 4000 25.1, 19.2 and 17.9; 1000 of 128 13.9, 11.7 and 12.1, 4000 17.5, 14.6 and 16.0, 12000 28.9, 21.3 and 19.1; 4000 of 60 12.1, 10.0
+  // and 10.1, 8000 15.1, 12.5 and 11.2, 16000 20.4, 15.4 and 14.0).
   int threads = 256;
   if (totals && tokens * lanes > 256 * 64) threads = tokens * lanes > kMostParts * 512 ? 1024 : 512;
   while (threads > 256 && threads / lanes * a.k > 6144) threads /= 2;  // 48 KiB of choices

@@ -62,6 +62,9 @@ inline Q8Shape q8_few_shape(const Q8Call& a, int x_tiles, bool own) {
   s.all_tiles = (wave_tiles + s.waves - 1) / s.waves;
   s.spread = s.all_tiles < 64 ? 0 : 3;
   s.tiles = ((s.all_tiles - 1) >> s.spread) + 1;
+  // Slots that have their turn with a workgroup's weights, which are then in the L2 (16 rows of x to a slot, in us by 1, 2, 4 and 8
+  // slots: 64 rows x 65536 x 8192 356, 257, 206, 206; 128 rows 710, 504, 405, 357; x 20000 x 4096 64 rows 49, 31, 28, 28).  Rows by expert
+  // have few slots to a matrix, and nothing to gain or lose (4096 rows on 128 experts of 1024 x 2048 83.5, 83.2, 80.8, 86.2).
   s.group = !s.spread ? 1 : a.sorted ? (a.rows > (int64_t)cols * a.experts ? 4 : 1) : slots < 8 ? slots : 8;
   s.grid = (s.tiles << s.spread) * s.group * ((slots + s.group - 1) / s.group);
   return s;
@@ -84,8 +87,9 @@ inline Q8Shape q8_tile_shape(const Q8Call& a, Q8Tile kind) {
 // to a CU.  With a shorter K the results' own time shows, `ends` ns for 16 x 16 of them, and the largest tiles take at
 // least `floor`.  Where the weights are more than the caches hold, memory's rate bounds all of them, `rate` in TB/s, at 1.5 times
 // the bytes with two tiles of x and so on in the kernel that streams (its tiles of x share weights in the L2 by half).
-// Fitted to 129 products in bf16 with every kernel, K from 80 to 10128: what it takes is 1 % slower than the fastest of the
-// seven on average, 33 % at most.  Some of them, in us by 16, 32, 64 and 128 rows of x in the streaming kernel, 256 x 64,
+// Fitted to 129 products in bf16 with every kernel, K from 80 to 10128: of these, what it takes is 1 % slower than the fastest
+// of the seven on average, 33 % at most.  An fp32 y and experts of uneven popularity are not among them; how the rows
+// lie over the experts it does not know.  Some of them, in us by 16, 32, 64 and 128 rows of x in the streaming kernel, 256 x 64,
 // 512 x 128 and 256 x 256:
 //   4096 x 4096: 64 rows 9.5, 9.9, 11.5, 24, 20.3, 48, 45; 256 rows 25, 16.7, 18.3, 27, 21, 50, 48; 512 rows 45, 30.5, 20, 28.5, 22.7,
 //     50, 48; 2048 rows 167, 88, 56, 63, 41, 56, 52

@@ -5,8 +5,9 @@
 // (4900 at 2.4 GHz with operands that never change; 32x32x32 ones 3430).  Of the about 2800 cycles
 // of a step of 128 columns (256 x 256 sums) 2092 are theirs; loads from LDS add 120, stores into it 360, loads from memory
 // 210, measured one by one.  Rows from memory straight into LDS were no faster (22 bytes a cycle of a CU, where the
-// way through registers has 70), nor operands two steps ahead in registers (spills).  8192 x 8192 x 8192 in bf16: 412 us, 2670
-// Tops, and about 420 in a run of many.  32768 x 4096 x 2048: 271 us, of which beginnings 30 and results 50.
+// way through registers has 70), nor operands two steps ahead in registers (spills).  8192 x 8192 x 8192 in bf16: 410 to 420 us,
+// 2620 to 2680 Tops, once the card's power control has settled; of 60 calls on a card idle before, the first four take 430 us, the next
+// fall back to 560 and recover within 50 (median 434 to 450).  32768 x 4096 x 2048: 271 us, of which beginnings 30 and results 50.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
